@@ -231,6 +231,107 @@ int bpdq_dequant_fp16(const uint32_t* planes, const uint16_t* coefs_h, int d_out
 int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits,
               int group, const float* x, float* y, void* stream);
 
+/* ---- serving side: the product for any number of tokens, with what surrounds it ---------------
+ * Y[t][r] = act( sum_c What[r][c] X[t][c] + bias[r] ) + residual[t][r],  What as in bpdq_dequant_fp16 (Eq. 1), straight
+ * from the stored planes and coefficients.
+ *   X : n_tok x d_in, row stride ldx;  bias : d_out or NULL;  residual : n_tok x d_out, row stride ldr, or NULL;
+ *   Y : n_tok x d_out, row stride ldy.  All of one type, BPDQ_F16 or BPDQ_BF16 (uint16 bit patterns); strides in elements.
+ *   act : BPDQ_ACT_*; GELU is v Phi(v), GELU_TANH its approximation by tanh, SILU v / (1 + exp(-v)).
+ * What is evaluated in fp32 and rounded once to the type of X; the products are exact, sums, bias, activation and residual
+ * fp32; Y is rounded once.  (A level of a row outside the range of BPDQ_F16 becomes infinite there; it does not in
+ * BPDQ_BF16.)  A NaN or infinity in a row of X reaches that row of Y alone.
+ * Y may be the residual itself (same address and stride); other overlaps are not allowed.  The result of a token does not
+ * depend on the others of the call beyond the choice of kernel by n_tok, which changes the order of sums.
+ * Requirements: d_in % 32 == 0, 32 | group | d_in; any alignment of the elements (X aligned to 16 bytes with ldx % 8 == 0,
+ * and planes likewise with d_in % 128 == 0, are quicker).  n_tok = 0 launches nothing.
+ * Returns 0, or a negative code naming the argument (-1 planes, -2 coefs_h, -3 d_out, -4 d_in, -5 bits, -6 group, -7 X,
+ * -8 n_tok, -9 ldx, -10 dtype, -11 bias, -12 act, -13 residual, -14 ldr, -15 Y, -16 ldy). */
+#define BPDQ_F32 0
+#define BPDQ_F16 1
+#define BPDQ_BF16 2
+#define BPDQ_ACT_NONE 0
+#define BPDQ_ACT_RELU 1
+#define BPDQ_ACT_GELU 2
+#define BPDQ_ACT_GELU_TANH 3
+#define BPDQ_ACT_SILU 4
+int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,
+                const void* X, int n_tok, long ldx, int dtype, const void* bias, int act,
+                const void* residual, long ldr, void* Y, long ldy, void* stream);
+
+/* ---- serving side: keys and values in 8 bits --------------------------------------------------
+ * The cache is in pages of `page` tokens.  A page and key head hold page * head_dim codes of K, as many of V, and one fp32
+ * scale of each; a value is (code - 128) * scale, code - 128 in [-127, 127].  Which page holds which tokens of which
+ * sequence is the caller's: row b of `page_table` (n_seq x max_pages ints) lists the pages of sequence b in order, so token
+ * t of it is slot t % page of page page_table[b][t / page].
+ * Layout of the head_dim * page bytes of a page and head: tiles of 64 tokens, in the order in which the matrix
+ * instructions take them; token t = 16 g + 4 u + i of a tile (g, u, i in 0..3):
+ *   K : [tile][u][d / 64][d % 64 / 16][g][i][d % 16]          V : [tile][d / 16][g][d % 16][t % 16]
+ */
+typedef struct bpdq_kv_cache {
+  uint8_t* k;          /* [n_pages][n_kv][page * head_dim], 16-byte aligned */
+  uint8_t* v;          /* likewise */
+  float* k_scale;      /* [n_pages][n_kv] */
+  float* v_scale;
+  int n_pages;
+  int n_kv;            /* key/value heads */
+  int page;            /* tokens per page: 64, 128 or 256 */
+  int head_dim;        /* 64, 128 or 256 */
+} bpdq_kv_cache;
+
+/* Quantizes new tokens into the cache.  Rows tok_start[b] .. tok_start[b+1]-1 of K and V (n_tok rows of n_kv heads of head_dim
+ * values, row strides ldk, ldv in elements, of type dtype: BPDQ_F32, BPDQ_F16 or BPDQ_BF16) become tokens pos[b] ... of
+ * sequence b.  max_tok: at least the largest count of a sequence.
+ * Scale and codes, per page and head, in fp32:
+ *   - the first slot of the page is among the new tokens: scale = max(amax, 2^-96) * (1/127), amax the largest magnitude of
+ *     the page's new tokens; what the page held before is gone.
+ *   - else the scale doubles until the new tokens fit: scale' = scale * 2^j, the smallest j >= 0 with amax <= 127 scale 2^j, and the
+ *     codes of the tokens before become rint((code - 128) / 2^j) + 128.  Doubling bounds what repeated rounding can do: however many
+ *     calls fill a page, no value is further than one step (scale) from what was written.
+ *   code = rint(x * (1 / scale)) + 128, ties to even, clamped to 1..255.
+ * A new token with a NaN or an infinity makes the scale of its page and head NaN, so all tokens of that page and head read as
+ * NaN until the page is written from its first slot again.  Slots behind the last token written hold no promise.
+ * A page must not belong to two sequences that the same call writes.  A sequence with pos < 0, tokens beyond max_pages pages, rows
+ * beyond n_tok and pages outside [0, n_pages) are left out.
+ * Requirements: k, v 16-byte aligned; n_seq <= 65535.  n_seq = 0, n_tok = 0 or max_tok = 0 launches nothing.
+ * Returns 0, or a negative code naming the argument (-1 cache, -2 page_table, -3 max_pages, -4 n_seq, -5 pos, -6 tok_start,
+ * -7 n_tok, -8 max_tok, -9 K, -10 ldk, -11 V, -12 ldv, -13 dtype). */
+int bpdq_kv_write(const bpdq_kv_cache* cache /* host */, const int* page_table, int max_pages, int n_seq,
+                  const int* pos, const int* tok_start, int n_tok, int max_tok, const void* K, long ldk,
+                  const void* V, long ldv, int dtype, void* stream);
+/* The inverse: tokens pos[b] .. of sequence b into rows tok_start[b] .. tok_start[b+1]-1 of K and V, (code - 128) * scale
+ * rounded to dtype.  Tokens that bpdq_kv_write would leave out read as zero (rows of a sequence with pos < 0 and rows that no
+ * sequence names are left alone).  Arguments and return codes as above. */
+int bpdq_kv_read(const bpdq_kv_cache* cache /* host */, const int* page_table, int max_pages, int n_seq,
+                 const int* pos, const int* tok_start, int n_tok, int max_tok, void* K, long ldk, void* V,
+                 long ldv, int dtype, void* stream);
+
+/* Attention of new tokens over the cache.  Sequence b has kv_len[b] tokens in the cache; its queries are rows q_start[b] ..
+ * q_start[b+1]-1 of Q (n_tok rows of n_q heads of head_dim values, row stride ldq), n of them, the last of them at position
+ * kv_len[b] - 1.  n_kv must divide n_q; query head h reads key head h / (n_q / n_kv).
+ *   out[i][h] = sum_t p_t v_t,  p = softmax over the visible t of scale * <q_i, k_t>
+ * Token t is visible to query i, at position p = kv_len - n + i, if t < kv_len, and t <= p where causal != 0, and t > p - window
+ * where window > 0.  A query that sees nothing gets zeros.  What is not visible is not looked at: neither its codes nor, on a page
+ * without visible tokens, the page's scale.
+ *   Q, out : BPDQ_F16 or BPDQ_BF16;  lse : NULL, or n_tok x n_q floats: log of the sum of exp(scale <q, k>), -inf for a query that
+ *   sees nothing.
+ *   max_q, max_kv : at least the largest count of queries and of cached tokens of a sequence; the work is laid out by them,
+ *   and longer sequences are cut to them.  max_kv <= max_pages * page.
+ * Scores and sums are fp32 on exact products (Q in bf16 is scaled by a power of two per row and head and taken as fp16, where a value
+ * below 2^-31 of the row's largest may lose bits); the unnormalised probabilities, at most 1, are rounded to fp16 for the
+ * product with V; out is rounded once.  A call's result does not change from run to run; the split of long caches depends on n_seq,
+ * max_q, n_q, n_kv, head_dim, max_kv and window alone.
+ * Pages outside [0, n_pages) count as not visible.
+ * Requirements: n_seq <= 65535; max_q * (n_q / n_kv) <= 2^24; ws 256-byte aligned, of bpdq_kv_attention_workspace_bytes() bytes
+ * (0 where nothing is split, ws may be NULL then).  out must not overlap Q.
+ * Returns 0, or a negative code naming the argument (-1 cache, -2 page_table, -3 max_pages, -4 n_seq, -5 kv_len, -6 q_start,
+ * -7 n_tok, -8 max_q, -9 max_kv, -10 Q, -11 ldq, -12 n_q, -13 dtype, -14 scale, -16 window, -17 out, -18 ldo, -20 ws,
+ * -21 ws_bytes). */
+size_t bpdq_kv_attention_workspace_bytes(int n_seq, int max_q, int max_kv, int n_q, int n_kv, int head_dim, int window);
+int bpdq_kv_attention(const bpdq_kv_cache* cache /* host */, const int* page_table, int max_pages, int n_seq,
+                      const int* kv_len, const int* q_start, int n_tok, int max_q, int max_kv, const void* Q,
+                      long ldq, int n_q, int dtype, float scale, int causal, int window, void* out, long ldo,
+                      float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- channel ordering around the pass (Sec. 4.1) --------------------------------------------
  * The pass quantizes the columns left to right; a caller that wants another order permutes W and
  * H first and carries `perm` with the stored layer.

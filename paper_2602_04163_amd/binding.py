@@ -25,6 +25,7 @@ EXPORTS = [
     "bpdq_channel_order_workspace_bytes", "bpdq_channel_order", "bpdq_channel_order_noalloc",
     "bpdq_gather_columns",
     "bpdq_scatter_columns", "bpdq_gather_symmetric", "bpdq_gemv",
+    "bpdq_linear", "bpdq_kv_write", "bpdq_kv_read", "bpdq_kv_attention_workspace_bytes", "bpdq_kv_attention",
     "bpdq_probe_mfma", "bpdq_probe_copy",
 ]
 
@@ -33,6 +34,12 @@ class BpdqParams(ctypes.Structure):
     _fields_ = [("bits", ctypes.c_int), ("group", ctypes.c_int), ("block", ctypes.c_int),
                 ("refine_iters", ctypes.c_int), ("alpha", ctypes.c_float),
                 ("grid", ctypes.c_int), ("coef_fp16", ctypes.c_int)]
+
+
+class BpdqKvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int), ("n_kv", ctypes.c_int),
+                ("page", ctypes.c_int), ("head_dim", ctypes.c_int)]
 
 
 class BpdqError(RuntimeError):
@@ -84,6 +91,16 @@ def load():
     lib.bpdq_coefs_to_fp16.argtypes = [vp, ctypes.c_long, vp, vp]
     lib.bpdq_gemv.restype = ci
     lib.bpdq_gemv.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp, vp]
+    cl, kv = ctypes.c_long, ctypes.POINTER(BpdqKvCache)
+    lib.bpdq_linear.restype = ci
+    lib.bpdq_linear.argtypes = [vp, vp, ci, ci, ci, ci, vp, ci, cl, ci, vp, ci, vp, cl, vp, cl, vp]
+    for name in ("bpdq_kv_write", "bpdq_kv_read"):
+        getattr(lib, name).restype = ci
+        getattr(lib, name).argtypes = [kv, vp, ci, ci, vp, vp, ci, ci, vp, cl, vp, cl, ci, vp]
+    lib.bpdq_kv_attention_workspace_bytes.restype = sz
+    lib.bpdq_kv_attention_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]
+    lib.bpdq_kv_attention.restype = ci
+    lib.bpdq_kv_attention.argtypes = [kv, vp, ci, ci, vp, vp, ci, ci, ci, vp, cl, ci, ci, cf, ci, ci, vp, cl, vp, vp, sz, vp]
     lib.bpdq_channel_order_workspace_bytes.restype = sz
     lib.bpdq_channel_order_workspace_bytes.argtypes = [ci]
     lib.bpdq_channel_order.restype = ci
@@ -415,6 +432,159 @@ def bpdq_gemv(planes, coefs_h, group, x, y=None):
     _check(lib.bpdq_gemv(_ptr(planes), _ptr(coefs_h), d_out, d_in, bits, group, _ptr(x), _ptr(y),
                          _stream()), "bpdq_gemv")
     return y
+
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _rows(t, dtype, shape, name):
+    """A tensor of the given shape on the GPU whose rows (all axes but the first) are dense."""
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+        raise BpdqError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
+    step = 1
+    for axis in range(t.dim() - 1, 0, -1):
+        if t.shape[axis] > 1 and t.stride(axis) != step:
+            raise BpdqError(f"{name}: its rows must be dense")
+        step *= t.shape[axis]
+    return max(t.stride(0), step) if t.shape[0] > 1 else step
+
+
+def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None, Y=None):
+    """Y = act(X What^T + bias) + residual from the stored format, for any number of tokens; X, bias, residual and Y float16 or
+    bfloat16.  Y may be the residual."""
+    lib = load()
+    _dev(planes, torch.int32, "planes")
+    _dev(coefs_h, torch.float16, "coefs_h")
+    bits, d_out, nw = planes.shape
+    d_in = nw * 32
+    if coefs_h.shape != (bits + 1, d_out, d_in // group):
+        raise BpdqError("coefs_h: expected (bits + 1) x d_out x (d_in / group)")
+    if X.dim() != 2 or X.dtype not in (torch.float16, torch.bfloat16):
+        raise BpdqError("X: expected a float16 or bfloat16 matrix")
+    if act not in ACTS:
+        raise BpdqError(f"act: expected one of {sorted(ACTS)}")
+    n_tok = X.shape[0]
+    ldx = _rows(X, X.dtype, (n_tok, d_in), "X")
+    if Y is None:
+        Y = torch.empty((n_tok, d_out), dtype=X.dtype, device=X.device)
+    ldy = _rows(Y, X.dtype, (n_tok, d_out), "Y")
+    if bias is not None:
+        _rows(bias, X.dtype, (d_out,), "bias")
+        if d_out > 1 and bias.stride(0) != 1:
+            raise BpdqError("bias: expected a dense vector")
+    ldr = 0 if residual is None else _rows(residual, X.dtype, (n_tok, d_out), "residual")
+    _check(lib.bpdq_linear(planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx,
+                           DTYPES[X.dtype], _ptr(bias), ACTS[act], _ptr(residual), ldr, Y.data_ptr(), ldy, _stream()),
+           "bpdq_linear")
+    return Y
+
+
+class KvCache:
+    """Keys and values in 8 bits: k, v uint8 (n_pages, n_kv, page, head_dim) in the layout of include/bpdq.h, k_scale, v_scale
+    float32 (n_pages, n_kv).  KvCache.empty(...) makes one."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "_c")
+
+    def __init__(self, k, v, k_scale, v_scale):
+        if k.dim() != 4:
+            raise BpdqError("k: expected n_pages x n_kv x page x head_dim")
+        for t, name in ((k, "k"), (v, "v")):
+            _dev(t, torch.uint8, name)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _dev(t, torch.float32, name)
+        if v.shape != k.shape or k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+            raise BpdqError("v as k, and scales of n_pages x n_kv, are expected")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        n_pages, n_kv, page, head_dim = k.shape
+        self._c = BpdqKvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages, n_kv, page, head_dim)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv, head_dim, page=64, device="cuda"):
+        shape = (n_pages, n_kv, page, head_dim)
+        return cls(torch.empty(shape, dtype=torch.uint8, device=device), torch.empty(shape, dtype=torch.uint8, device=device),
+                   torch.empty(shape[:2], device=device), torch.empty(shape[:2], device=device))
+
+
+def _sequences(cache, page_table, at, start):
+    """Checks of what describes the sequences of a call; their number and the table's width."""
+    _dev(page_table, torch.int32, "page_table")
+    _dev(at, torch.int32, "pos / kv_len")
+    _dev(start, torch.int32, "tok_start / q_start")
+    n_seq = at.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != n_seq or start.numel() != n_seq + 1:
+        raise BpdqError("page_table: expected n_seq x max_pages, and n_seq + 1 starts")
+    return n_seq, page_table.shape[1]
+
+
+def bpdq_kv_write(cache, page_table, pos, tok_start, K, V, max_tok=None):
+    """Quantizes rows tok_start[b] .. tok_start[b+1]-1 of K and V (n_tok, n_kv, head_dim) into the cache as tokens pos[b] .. of
+    sequence b.  max_tok: at least the largest count of a sequence (all rows, if it is not given)."""
+    n_seq, max_pages = _sequences(cache, page_table, pos, tok_start)
+    c = cache._c
+    n_tok = K.shape[0]
+    shape = (n_tok, c.n_kv, c.head_dim)
+    if K.dtype not in DTYPES:
+        raise BpdqError("K: expected float32, float16 or bfloat16")
+    ldk, ldv = _rows(K, K.dtype, shape, "K"), _rows(V, K.dtype, shape, "V")
+    _check(load().bpdq_kv_write(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(),
+                                n_tok, n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv,
+                                DTYPES[K.dtype], _stream()), "bpdq_kv_write")
+
+
+def bpdq_kv_read(cache, page_table, pos, tok_start, n_tok, max_tok=None, dtype=torch.float32, K=None, V=None):
+    """Tokens pos[b] .. of sequence b from the cache into rows tok_start[b] .. tok_start[b+1]-1 of K and V; returns both."""
+    n_seq, max_pages = _sequences(cache, page_table, pos, tok_start)
+    c = cache._c
+    shape = (n_tok, c.n_kv, c.head_dim)
+    if dtype not in DTYPES:
+        raise BpdqError("dtype: expected float32, float16 or bfloat16")
+    if K is None:
+        K = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    if V is None:
+        V = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    ldk, ldv = _rows(K, dtype, shape, "K"), _rows(V, dtype, shape, "V")
+    _check(load().bpdq_kv_read(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(),
+                               n_tok, n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv,
+                               DTYPES[dtype], _stream()), "bpdq_kv_read")
+    return K, V
+
+
+def bpdq_kv_attention_workspace_bytes(n_seq, max_q, max_kv, n_q, n_kv, head_dim, window=0):
+    return load().bpdq_kv_attention_workspace_bytes(n_seq, max_q, max_kv, n_q, n_kv, head_dim, window)
+
+
+def bpdq_kv_attention(cache, page_table, kv_len, q_start, Q, max_q=None, max_kv=None, scale=None, causal=True, window=0,
+                      out=None, lse=None, ws=None):
+    """Attention of rows q_start[b] .. q_start[b+1]-1 of Q (n_tok, n_q, head_dim), the last of them at position kv_len[b] - 1, over
+    the kv_len[b] cached tokens of sequence b.  max_q, max_kv: at least the largest counts (all rows and all of the table's
+    pages, if they are not given); scale: 1 / sqrt(head_dim) by default; lse: float32 (n_tok, n_q), filled if given."""
+    lib = load()
+    n_seq, max_pages = _sequences(cache, page_table, kv_len, q_start)
+    c = cache._c
+    if Q.dim() != 3 or Q.dtype not in (torch.float16, torch.bfloat16):
+        raise BpdqError("Q: expected a float16 or bfloat16 tensor of n_tok x n_q x head_dim")
+    n_tok, n_q = Q.shape[:2]
+    shape = (n_tok, n_q, c.head_dim)
+    ldq = _rows(Q, Q.dtype, shape, "Q")
+    if max_q is None:
+        max_q = n_tok
+    if max_kv is None:
+        max_kv = max_pages * c.page
+    if out is None:
+        out = torch.empty(shape, dtype=Q.dtype, device=Q.device)
+    ldo = _rows(out, Q.dtype, shape, "out")
+    if lse is not None:
+        _dev(lse, torch.float32, "lse")
+        if lse.shape != (n_tok, n_q):
+            raise BpdqError("lse: expected n_tok x n_q")
+    if ws is None:
+        need = lib.bpdq_kv_attention_workspace_bytes(n_seq, max_q, max_kv, n_q, c.n_kv, c.head_dim, window)
+        ws = _workspace(need, Q.device) if need else None
+    _check(lib.bpdq_kv_attention(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, kv_len.data_ptr(),
+                                 q_start.data_ptr(), n_tok, max_q, max_kv, Q.data_ptr(), ldq, n_q, DTYPES[Q.dtype],
+                                 c.head_dim ** -0.5 if scale is None else scale, int(bool(causal)), window, out.data_ptr(), ldo,
+                                 _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()), "bpdq_kv_attention")
+    return out
 
 
 PROBE_KINDS = {"f32": 0, "bf16": 1, "f16": 2, "f64": 3, "i8": 4}

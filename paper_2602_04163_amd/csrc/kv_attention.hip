@@ -1,0 +1,464 @@
+// Attention of new tokens over the 8-bit key/value cache:
+//   out_r = sum_t p_t v_t / l,   p_t = exp(z_t - m),  z_t = scale <q_r, k_t>,  m = max z_t,  l = sum p_t
+// in one pass over the cache with the running maximum and sum: after a tile of 64 tokens m' = max(m, tile), and l and the sums
+// of p v are scaled by exp(m - m') before the tile's terms are added.
+//
+// A row r of a work item is a (query, head) pair of one key head: the G = n_q / n_kv heads that share it and, where a sequence
+// brings several tokens, those tokens too, so that the cache is read once for all of them.
+//
+// Products.  Everything is computed transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds scores of one row (column
+// l % 16 of the 16 x 16 tiles) and 16 tokens of a tile (16 (l / 16) ..), which is at the same time the operand layout that the
+// second product wants of P^T, so P never leaves its registers, and a row's maximum and sum cross lanes twice only.  The token
+// order inside a tile and the channel order inside the first product are free; the cache's layout is the one in which every load is 16 bytes
+// a lane and 1 KB of consecutive bytes a wavefront.  A code byte becomes an fp16 by v_perm_b32 with 0x64 (1024 + code) and a
+// packed subtraction of 1152, both exact.  The scale of K multiplies the scores, that of V a tile's share of O, in fp32.
+//
+// Work-group: four wavefronts that take the tiles of a chunk in turn, each with its own m, l and O, joined in LDS in a fixed
+// order.  Long caches are cut into chunks, whose unnormalised O, m and l go to the workspace; a second launch joins them.
+#include "kv_cache.h"
+
+namespace bpdq {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kAttnThreads = 256;
+constexpr int kAttnWaves = kAttnThreads / 64;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+struct AttnArgs {
+  bpdq_kv_cache c;
+  const int* table;
+  const int* kv_len;
+  const int* q_start;
+  const void* q;
+  void* out;
+  float* lse;
+  float* part;                                           // [item][chunk][rows][dim] sums, then [item][chunk][rows][2] m, l
+  long ldq, ldo;
+  int max_pages, n_tok, max_q, max_kv, n_q, group;
+  int causal, window;
+  int q_tiles, n_chunk, chunk_tiles;
+  float scale;
+};
+
+// One work item: rows r0 .. of a sequence and key head, and the tiles of the cache that any of them sees.
+struct AttnItem {
+  int first, q_len, rows, r0, kv;
+  int tile_lo, tile_hi;                                  // tiles tile_lo .. tile_hi - 1
+  bool there;
+};
+
+template <int ROWS>
+__device__ __forceinline__ AttnItem attn_item(const AttnArgs& a, int seq, int q_tile) {
+  AttnItem it;
+  it.first = a.q_start[seq];
+  long n = (long)a.q_start[seq + 1] - it.first;
+  n = n < a.max_q ? n : a.max_q;
+  n = n < (long)a.n_tok - it.first ? n : (long)a.n_tok - it.first;
+  it.there = false;
+  if (it.first < 0 || n <= 0) return it;
+  it.q_len = (int)n;
+  it.rows = it.q_len * a.group;
+  it.r0 = q_tile * ROWS;
+  if (it.r0 >= it.rows) return it;
+  it.there = true;
+  int kv = a.kv_len[seq];
+  kv = kv < 0 ? 0 : kv;
+  it.kv = kv < a.max_kv ? kv : a.max_kv;
+  const int last = (it.rows < it.r0 + ROWS ? it.rows : it.r0 + ROWS) - 1;
+  const int off = it.kv - it.q_len;
+  int hi = it.kv - 1, lo = 0;
+  if (a.causal) hi = off + last / a.group < hi ? off + last / a.group : hi;
+  if (a.window > 0) lo = off + it.r0 / a.group - a.window + 1 > 0 ? off + it.r0 / a.group - a.window + 1 : 0;
+  it.tile_lo = lo / kKvTile;
+  it.tile_hi = hi >= lo ? hi / kKvTile + 1 : it.tile_lo;
+  return it;
+}
+
+__device__ __forceinline__ int attn_chunks(const AttnItem& it, int chunk_tiles) {
+  const int n = bpdq_ceil_div(it.tile_hi - it.tile_lo, chunk_tiles);
+  return n > 0 ? n : 1;
+}
+
+// eight codes (bytes of two words) as fp16
+__device__ __forceinline__ f16x8_t attn_codes(uint32_t a, uint32_t b) {
+  const uint32_t w[4] = {__builtin_amdgcn_perm(0x64646464u, a, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u),
+                         __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)};
+  const f16x2_t zero = {(_Float16)1152.f, (_Float16)1152.f};
+  f16x8_t out;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const f16x2_t v = __builtin_bit_cast(f16x2_t, w[q]) - zero;
+    out[2 * q] = v[0];
+    out[2 * q + 1] = v[1];
+  }
+  return out;
+}
+
+// T: type of Q and out;  D: head dimension;  NQ: tiles of 16 rows.
+template <typename T, int D, int NQ>
+__global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
+  constexpr int ROWS = 16 * NQ, C = D / 64, DT = D / 16, kAcc = D + 4;
+  __shared__ float acc_s[ROWS * kAcc];
+  __shared__ float m_s[kAttnWaves][ROWS], l_s[kAttnWaves][ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int chunk = blockIdx.x % a.n_chunk;
+  const int item = blockIdx.x / a.n_chunk;               // (head, query tile)
+  const int h = item % a.c.n_kv, q_tile = item / a.c.n_kv, seq = blockIdx.y;
+  const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
+  if (!it.there) return;                                 // uniform
+  const int n_chunk = attn_chunks(it, a.chunk_tiles);
+  if (chunk >= n_chunk) return;
+  const int t_begin = it.tile_lo + chunk * a.chunk_tiles;
+  const int t_end = it.tile_hi < t_begin + a.chunk_tiles ? it.tile_hi : t_begin + a.chunk_tiles;
+
+  // the rows' queries as operands: channel 64 c + 16 quarter + 8 s + j is k = 8 quarter + j of product (c, s)
+  f16x8_t qf[NQ][C][2];
+  float q_scale[NQ];                                     // of the scores, to base 2
+  int see_lo[NQ], see_hi[NQ];                            // tokens that the lane's row sees: see_lo <= t < see_hi
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = it.r0 + 16 * n + col;
+    const bool on = r < it.rows;
+    const int i = (on ? r : 0) / a.group, head = h * a.group + (on ? r : 0) % a.group;
+    const T* q = static_cast<const T*>(a.q) + (long)(it.first + i) * a.ldq + (long)head * D;
+    float most = 0.f;
+    T x[C][16];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[c][e] = q[64 * c + 16 * quarter + e];
+        most = fmaxf(most, fabsf((float)x[c][e]));
+      }
+    float f = 1.f, back = 1.f;
+    if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
+      most = fmaxf(most, __shfl_xor(most, 16, 64));
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      if (most > 0.f && most < __builtin_huge_valf()) {  // into [2^14, 2^15)
+        int e;
+        (void)frexpf(most, &e);
+        e = 15 - e < 126 ? 15 - e : 126;
+        f = ldexpf(1.f, e);
+        back = ldexpf(1.f, -e);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) qf[n][c][e / 8][e % 8] = (_Float16)((float)x[c][e] * f);
+    q_scale[n] = back * (a.scale * kLog2e);
+    const int p = it.kv - it.q_len + i;
+    see_lo[n] = a.window > 0 ? p - a.window + 1 : 0;
+    see_hi[n] = !on ? 0 : a.causal && p + 1 < it.kv ? p + 1 : it.kv;
+  }
+
+  f32x4_t o[NQ][DT];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m[n] = -__builtin_huge_valf();
+    l[n] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int per_page = a.c.page / kKvTile;
+  for (int tile = t_begin + wave; tile < t_end; tile += kAttnWaves) {
+    const int page = tile / per_page;
+    const int id = a.table[(long)seq * a.max_pages + page];
+    if (id < 0 || id >= a.c.n_pages) continue;           // uniform
+    const long at = (long)id * a.c.n_kv + h;
+    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(a.c.k + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(a.c.v + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+    const float k_scale = a.c.k_scale[at];
+    float v_scale = a.c.v_scale[at];
+    f32x4_t s[NQ][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s[n][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const u32x4_t w = kp[(u * C + c) * 64];
+        const f16x8_t k0 = attn_codes(w[0], w[1]), k1 = attn_codes(w[2], w[3]);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[n][c][0], s[n][u], 0, 0, 0);
+          s[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[n][c][1], s[n][u], 0, 0, 0);
+        }
+      }
+    }
+    // values of a page whose scale is not finite reach the rows that see them, and no others: by the probabilities
+    const bool bad = !(fabsf(v_scale) < __builtin_huge_valf());
+    if (bad) v_scale = 1.f;
+    f16x8_t p[NQ][2];
+    float fade[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const float f = k_scale * q_scale[n];
+      const int t0 = tile * kKvTile + 16 * quarter;
+      float top = m[n];
+      bool seen[4][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + 4 * u + i;
+          seen[u][i] = t >= see_lo[n] && t < see_hi[n];
+          s[n][u][i] = seen[u][i] ? s[n][u][i] * f : -__builtin_huge_valf();
+          top = fmaxf(top, s[n][u][i]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float base = top == -__builtin_huge_valf() ? 0.f : top;
+      fade[n] = __builtin_amdgcn_exp2f(m[n] - base);
+      m[n] = top;
+      l[n] *= fade[n];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float e = __builtin_amdgcn_exp2f(s[n][u][i] - base);
+          if (bad && seen[u][i]) e = __builtin_nanf("");
+          l[n] += e;
+          p[n][u / 2][4 * (u % 2) + i] = (_Float16)e;
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const u32x4_t w = vp[d * 64];
+      const f16x8_t v0 = attn_codes(w[0], w[1]), v1 = attn_codes(w[2], w[3]);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        f32x4_t pv = {0.f, 0.f, 0.f, 0.f};
+        pv = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][0], pv, 0, 0, 0);
+        pv = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[n][1], pv, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][d][i] = fmaf(o[n][d][i], fade[n], v_scale * pv[i]);
+      }
+    }
+  }
+
+  // join the wavefronts
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    l[n] += __shfl_xor(l[n], 16, 64);
+    l[n] += __shfl_xor(l[n], 32, 64);
+    if (lane < 16) {
+      m_s[wave][16 * n + col] = m[n];
+      l_s[wave][16 * n + col] = l[n];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float top = m_s[0][16 * n + col];
+#pragma unroll
+    for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, m_s[w][16 * n + col]);
+    // a wavefront that saw nothing has zero sums (or a NaN, which stays)
+    const float f = m[n] == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m[n] - top);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[n][d][i] *= f;
+  }
+  for (int w = 0; w < kAttnWaves; ++w) {
+    if (wave == w) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f32x4_t* at = reinterpret_cast<f32x4_t*>(acc_s + (16 * n + col) * kAcc + 16 * d + 4 * quarter);
+          *at = w ? *at + o[n][d] : o[n][d];
+        }
+    }
+    __syncthreads();
+  }
+  const int out_rows = it.rows - it.r0 < ROWS ? it.rows - it.r0 : ROWS;
+  const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk + chunk;
+  const long n_slot = (long)gridDim.y * a.q_tiles * a.c.n_kv * a.n_chunk;
+  for (int id = tid; id < out_rows * (D / 4); id += kAttnThreads) {
+    const int r = id / (D / 4), d = 4 * (id % (D / 4));
+    float top = m_s[0][r];
+#pragma unroll
+    for (int w = 1; w < kAttnWaves; ++w) top = fmaxf(top, m_s[w][r]);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kAttnWaves; ++w)
+      sum += l_s[w][r] * (m_s[w][r] == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m_s[w][r] - top));
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(acc_s + r * kAcc + d);
+    if (n_chunk > 1) {
+      *reinterpret_cast<f32x4_t*>(a.part + (slot * ROWS + r) * D + d) = v;
+      if (d == 0) {
+        float* ml = a.part + n_slot * ROWS * D + (slot * ROWS + r) * 2;
+        ml[0] = top;
+        ml[1] = sum;
+      }
+    } else {
+      const int i = (it.r0 + r) / a.group, head = h * a.group + (it.r0 + r) % a.group;
+      T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D + d;
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[e] = (T)(v[e] * f);
+      if (a.lse && d == 0)
+        a.lse[(long)(it.first + i) * a.n_q + head] = sum == 0.f ? -__builtin_huge_valf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+  }
+}
+
+// Joins the chunks of a work item, in order.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
+  const int h = blockIdx.x % a.c.n_kv, q_tile = blockIdx.x / a.c.n_kv, seq = blockIdx.y;
+  const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
+  if (!it.there) return;
+  const int n_chunk = attn_chunks(it, a.chunk_tiles);
+  if (n_chunk <= 1) return;                              // written by the first launch
+  const int out_rows = it.rows - it.r0 < ROWS ? it.rows - it.r0 : ROWS;
+  const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk;
+  const long n_slot = (long)gridDim.y * a.q_tiles * a.c.n_kv * a.n_chunk;
+  const float* ml = a.part + n_slot * ROWS * D + slot * ROWS * 2;
+  for (int id = threadIdx.x + blockIdx.z * kAttnThreads; id < out_rows * (D / 4); id += kAttnThreads * gridDim.z) {
+    const int r = id / (D / 4), d = 4 * (id % (D / 4));
+    float top = -__builtin_huge_valf();
+    for (int c = 0; c < n_chunk; ++c) top = fmaxf(top, ml[((long)c * ROWS + r) * 2]);
+    float sum = 0.f;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < n_chunk; ++c) {
+      const float mc = ml[((long)c * ROWS + r) * 2], lc = ml[((long)c * ROWS + r) * 2 + 1];
+      const float f = mc == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(mc - top);
+      sum = fmaf(lc, f, sum);
+      const f32x4_t part = *reinterpret_cast<const f32x4_t*>(a.part + ((slot + c) * ROWS + r) * D + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(part[e], f, v[e]);
+    }
+    const int i = (it.r0 + r) / a.group, head = h * a.group + (it.r0 + r) % a.group;
+    T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D + d;
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = (T)(v[e] * f);
+    if (a.lse && d == 0)
+      a.lse[(long)(it.first + i) * a.n_q + head] = sum == 0.f ? -__builtin_huge_valf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  }
+}
+
+// How a call is laid out: rows to a work item, work items along the queries, chunks along the cache.
+struct AttnPlan {
+  int rows, q_tiles, n_chunk, chunk_tiles;
+  size_t ws_bytes;
+};
+
+// A window that reaches over every cache is none.
+static int attn_window(int window, int max_kv) { return window < max_kv ? window : 0; }
+
+static AttnPlan attn_plan(int n_seq, int max_q, int max_kv, int n_q, int n_kv, int dim, int window) {
+  AttnPlan p;
+  const long rows = (long)max_q * (n_q / n_kv);
+  p.rows = rows <= 16 ? 16 : 32;
+  p.q_tiles = (int)((rows + p.rows - 1) / p.rows);
+  // tiles that a work item can see
+  window = attn_window(window, max_kv);
+  long span = max_kv;
+  if (window > 0 && window + (long)max_q < span) span = window + (long)max_q;
+  const int tiles = (int)((span + kKvTile - 1) / kKvTile) + (window > 0 ? 1 : 0);
+  // 1024 work-groups, four to a CU, with at least eight tiles each
+  const long items = (long)n_seq * n_kv * p.q_tiles;
+  long n = (1024 + items - 1) / items;
+  n = n < tiles / 8 ? n : tiles / 8;
+  n = n > 1 ? n : 1;
+  p.chunk_tiles = bpdq_ceil_div(bpdq_ceil_div(tiles > 0 ? tiles : 1, (int)n), kAttnWaves) * kAttnWaves;
+  p.n_chunk = bpdq_ceil_div(tiles > 0 ? tiles : 1, p.chunk_tiles);
+  p.ws_bytes = p.n_chunk > 1 ? (size_t)items * p.n_chunk * p.rows * (dim + 2) * sizeof(float) : 0;
+  return p;
+}
+
+template <typename T, int D>
+static int attn_launch(const AttnArgs& a, const AttnPlan& p, int n_seq, hipStream_t stream) {
+  const dim3 grid((unsigned)(p.q_tiles * a.c.n_kv * p.n_chunk), n_seq);
+  if (p.rows == 16) hipLaunchKernelGGL((attn_rows_kernel<T, D, 1>), grid, dim3(kAttnThreads), 0, stream, a);
+  else hipLaunchKernelGGL((attn_rows_kernel<T, D, 2>), grid, dim3(kAttnThreads), 0, stream, a);
+  BPDQ_LAUNCH_CHECK();
+  if (p.n_chunk > 1) {
+    const dim3 join((unsigned)(p.q_tiles * a.c.n_kv), n_seq, bpdq_ceil_div(p.rows * (D / 4), kAttnThreads));
+    if (p.rows == 16) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), join, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_join_kernel<T, D, 32>), join, dim3(kAttnThreads), 0, stream, a);
+    BPDQ_LAUNCH_CHECK();
+  }
+  return 0;
+}
+
+template <typename T>
+static int attn_by_dim(const AttnArgs& a, const AttnPlan& p, int n_seq, hipStream_t stream) {
+  switch (a.c.head_dim) {
+    case 64: return attn_launch<T, 64>(a, p, n_seq, stream);
+    case 128: return attn_launch<T, 128>(a, p, n_seq, stream);
+    default: return attn_launch<T, 256>(a, p, n_seq, stream);
+  }
+}
+
+}  // namespace bpdq
+
+using namespace bpdq;
+
+extern "C" size_t bpdq_kv_attention_workspace_bytes(int n_seq, int max_q, int max_kv, int n_q, int n_kv, int head_dim, int window) {
+  if (n_seq <= 0 || max_q <= 0 || max_kv <= 0 || n_kv <= 0 || n_q <= 0 || n_q % n_kv || window < 0 ||
+      (head_dim != 64 && head_dim != 128 && head_dim != 256) || (long)max_q * (n_q / n_kv) > (1L << 24))
+    return 0;
+  return attn_plan(n_seq, max_q, max_kv, n_q, n_kv, head_dim, window).ws_bytes;
+}
+
+extern "C" int bpdq_kv_attention(const bpdq_kv_cache* cache, const int* page_table, int max_pages, int n_seq, const int* kv_len,
+                                 const int* q_start, int n_tok, int max_q, int max_kv, const void* Q, long ldq, int n_q,
+                                 int dtype, float scale, int causal, int window, void* out, long ldo, float* lse, void* ws,
+                                 size_t ws_bytes, void* stream_) {
+  if (!kv_cache_ok(cache)) return -1;
+  if (max_pages <= 0) return -3;
+  if (n_seq < 0 || n_seq > 65535) return -4;
+  if (n_tok < 0) return -7;
+  if (n_q <= 0 || n_q % cache->n_kv) return -12;
+  const int group = n_q / cache->n_kv;
+  if (max_q < 0 || (long)max_q * group > (1L << 24)) return -8;
+  if (max_kv < 0 || max_kv > (long)max_pages * cache->page) return -9;
+  if (dtype != BPDQ_F16 && dtype != BPDQ_BF16) return -13;
+  if (!(scale - scale == 0.f)) return -14;
+  if (window < 0) return -16;
+  if (n_seq == 0 || n_tok == 0 || max_q == 0) return 0;
+  const long row = (long)n_q * cache->head_dim;
+  if (!page_table) return -2;
+  if (!kv_len) return -5;
+  if (!q_start) return -6;
+  if (!Q || (reinterpret_cast<uintptr_t>(Q) & 1)) return -10;
+  if (ldq < row) return -11;
+  if (!out || (reinterpret_cast<uintptr_t>(out) & 1)) return -17;
+  if (ldo < row) return -18;
+  const AttnPlan p = attn_plan(n_seq, max_q, max_kv, n_q, cache->n_kv, cache->head_dim, window);
+  if ((long)p.q_tiles * cache->n_kv * p.n_chunk * kAttnThreads > 0xffffffffL) return -8;      // threads along the grid's x
+  if (p.ws_bytes && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))) return -20;
+  if (ws_bytes < p.ws_bytes) return -21;
+  AttnArgs a;
+  a.c = *cache;
+  a.table = page_table;
+  a.kv_len = kv_len;
+  a.q_start = q_start;
+  a.q = Q;
+  a.out = out;
+  a.lse = lse;
+  a.part = static_cast<float*>(ws);
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.max_pages = max_pages;
+  a.n_tok = n_tok;
+  a.max_q = max_q;
+  a.max_kv = max_kv;
+  a.n_q = n_q;
+  a.group = group;
+  a.causal = causal != 0;
+  a.window = attn_window(window, max_kv);
+  a.q_tiles = p.q_tiles;
+  a.n_chunk = p.n_chunk;
+  a.chunk_tiles = p.chunk_tiles;
+  a.scale = scale;
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  return dtype == BPDQ_F16 ? attn_by_dim<_Float16>(a, p, n_seq, stream) : attn_by_dim<__bf16>(a, p, n_seq, stream);
+}
