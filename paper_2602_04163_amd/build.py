@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbpdq.so")
 # the heaviest translation units first: the pool starts them first
-SOURCES = ["group_sweep_k3_g256.hip",
+SOURCES = ["linear_k4.hip", "linear_k3.hip", "linear_k2.hip", "linear_k1.hip", "group_sweep_k3_g256.hip",
            "group_sweep_k3_g256u.hip", "group_sweep_k2_g256.hip", "group_sweep_k2_g256u.hip",
            "group_sweep_k1_g256.hip", "group_sweep_k1_g256u.hip", "group_sweep_k4.hip",
            "group_sweep_k3.hip", "group_sweep_k2.hip", "group_sweep_k1.hip", "hessian.hip", "prepare.hip", "quantize.hip", "order.hip", "gemv.hip", "linear.hip",
