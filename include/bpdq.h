@@ -242,10 +242,12 @@ int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_
  * BPDQ_BF16.)  A NaN or infinity in a row of X reaches that row of Y alone.
  * Y may be the residual itself (same address and stride); other overlaps are not allowed.  The result of a token does not
  * depend on the others of the call beyond the choice of kernel by n_tok, which changes the order of sums.
+ * From 33 tokens on X is brought into the order of the matrix instructions first, in ws: 256-byte aligned,
+ * bpdq_linear_workspace_bytes() bytes (0 for fewer tokens, ws may be NULL then).
  * Requirements: d_in % 32 == 0, 32 | group | d_in; any alignment of the elements (X aligned to 16 bytes with ldx % 8 == 0,
  * and planes likewise with d_in % 128 == 0, are quicker).  n_tok = 0 launches nothing.
  * Returns 0, or a negative code naming the argument (-1 planes, -2 coefs_h, -3 d_out, -4 d_in, -5 bits, -6 group, -7 X,
- * -8 n_tok, -9 ldx, -10 dtype, -11 bias, -12 act, -13 residual, -14 ldr, -15 Y, -16 ldy). */
+ * -8 n_tok, -9 ldx, -10 dtype, -11 bias, -12 act, -13 residual, -14 ldr, -15 Y, -16 ldy, -17 ws, -18 ws_bytes). */
 #define BPDQ_F32 0
 #define BPDQ_F16 1
 #define BPDQ_BF16 2
@@ -254,9 +256,10 @@ int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_
 #define BPDQ_ACT_GELU 2
 #define BPDQ_ACT_GELU_TANH 3
 #define BPDQ_ACT_SILU 4
+size_t bpdq_linear_workspace_bytes(int n_tok, int d_in);
 int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,
                 const void* X, int n_tok, long ldx, int dtype, const void* bias, int act,
-                const void* residual, long ldr, void* Y, long ldy, void* stream);
+                const void* residual, long ldr, void* Y, long ldy, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- serving side: keys and values in 8 bits --------------------------------------------------
  * The cache is in pages of `page` tokens.  A page and key head hold page * head_dim codes of K, as many of V, and one fp32

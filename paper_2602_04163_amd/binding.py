@@ -25,7 +25,7 @@ EXPORTS = [
     "bpdq_channel_order_workspace_bytes", "bpdq_channel_order", "bpdq_channel_order_noalloc",
     "bpdq_gather_columns",
     "bpdq_scatter_columns", "bpdq_gather_symmetric", "bpdq_gemv",
-    "bpdq_linear", "bpdq_kv_write", "bpdq_kv_read", "bpdq_kv_attention_workspace_bytes", "bpdq_kv_attention",
+    "bpdq_linear_workspace_bytes", "bpdq_linear", "bpdq_kv_write", "bpdq_kv_read", "bpdq_kv_attention_workspace_bytes", "bpdq_kv_attention",
     "bpdq_probe_mfma", "bpdq_probe_copy",
 ]
 
@@ -93,7 +93,9 @@ def load():
     lib.bpdq_gemv.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp, vp]
     cl, kv = ctypes.c_long, ctypes.POINTER(BpdqKvCache)
     lib.bpdq_linear.restype = ci
-    lib.bpdq_linear.argtypes = [vp, vp, ci, ci, ci, ci, vp, ci, cl, ci, vp, ci, vp, cl, vp, cl, vp]
+    lib.bpdq_linear.argtypes = [vp, vp, ci, ci, ci, ci, vp, ci, cl, ci, vp, ci, vp, cl, vp, cl, vp, sz, vp]
+    lib.bpdq_linear_workspace_bytes.restype = sz
+    lib.bpdq_linear_workspace_bytes.argtypes = [ci, ci]
     for name in ("bpdq_kv_write", "bpdq_kv_read"):
         getattr(lib, name).restype = ci
         getattr(lib, name).argtypes = [kv, vp, ci, ci, vp, vp, ci, ci, vp, cl, vp, cl, ci, vp]
@@ -450,7 +452,11 @@ def _rows(t, dtype, shape, name):
     return max(t.stride(0), step) if t.shape[0] > 1 else step
 
 
-def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None, Y=None):
+def bpdq_linear_workspace_bytes(n_tok, d_in):
+    return load().bpdq_linear_workspace_bytes(n_tok, d_in)
+
+
+def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None, Y=None, ws=None):
     """Y = act(X What^T + bias) + residual from the stored format, for any number of tokens; X, bias, residual and Y float16 or
     bfloat16.  Y may be the residual."""
     lib = load()
@@ -473,9 +479,12 @@ def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None,
         _rows(bias, X.dtype, (d_out,), "bias")
         if d_out > 1 and bias.stride(0) != 1:
             raise BpdqError("bias: expected a dense vector")
+    if ws is None and n_tok > 32:
+        ws = _workspace(lib.bpdq_linear_workspace_bytes(n_tok, d_in), X.device)
     ldr = 0 if residual is None else _rows(residual, X.dtype, (n_tok, d_out), "residual")
     _check(lib.bpdq_linear(planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx,
-                           DTYPES[X.dtype], _ptr(bias), ACTS[act], _ptr(residual), ldr, Y.data_ptr(), ldy, _stream()),
+                           DTYPES[X.dtype], _ptr(bias), ACTS[act], _ptr(residual), ldr, Y.data_ptr(), ldy, _ptr(ws),
+                           0 if ws is None else ws.numel(), _stream()),
            "bpdq_linear")
     return Y
 

@@ -9,12 +9,17 @@
 #pragma once
 #include "planes.h"
 
+#include <type_traits>
+
 namespace bpdq {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kLinRowsMost = 32;                           // tokens of the kernel without an ordering of X
+constexpr int kLinTokPad = 256;                           // the ordering covers whole tiles of any shape
 
 struct LinearArgs {
   const uint32_t* planes;
@@ -23,6 +28,7 @@ struct LinearArgs {
   const void* bias;
   const void* residual;
   void* y;
+  void* ws;                                              // X in the order of the tile kernel
   long ldx, ldr, ldy;
   int d_out, d_in, group, n_tok, act;
   int vec_x, vec_w, vec_r, vec_y;                        // whether X, the planes, the residual and Y go by 16 bytes
@@ -36,16 +42,32 @@ __device__ __forceinline__ f32x4_t mfma_16x16x32(u32x4_t a, u32x4_t b, f32x4_t c
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+template <int ACT>
+__device__ __forceinline__ float linear_act(float v) {
+  if constexpr (ACT == BPDQ_ACT_RELU) return v > 0.f ? v : (v == v ? 0.f : v);
+  if constexpr (ACT == BPDQ_ACT_GELU) {
+    // v Phi(v), with erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x) for x >= 0 (Abramowitz and Stegun 7.1.26, absolute
+    // error below 1.5e-7): Phi(v) = erfc(-v / sqrt 2) / 2 below zero and 1 - erfc(v / sqrt 2) / 2 above
+    const float x = fabsf(v) * 0.70710678118654752440f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * poly * __expf(-x * x);
+    return v * (v < 0.f ? tail : 1.f - tail);
+  }
+  if constexpr (ACT == BPDQ_ACT_GELU_TANH) {
+    // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2u))
+    const float u = 0.79788456080286535588f * (v + 0.044715f * v * v * v);
+    return v * __builtin_amdgcn_rcpf(1.f + __expf(-2.f * u));
+  }
+  if constexpr (ACT == BPDQ_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
+  return v;
+}
 __device__ __forceinline__ float linear_act(float v, int act) {
   switch (act) {
-    case BPDQ_ACT_RELU: return v > 0.f ? v : (v == v ? 0.f : v);
-    case BPDQ_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752440f));
-    case BPDQ_ACT_GELU_TANH: {
-      // 1 + tanh(u) = 2 / (1 + exp(-2u))
-      const float u = 0.79788456080286535588f * (v + 0.044715f * v * v * v);
-      return v / (1.f + __expf(-2.f * u));
-    }
-    case BPDQ_ACT_SILU: return v / (1.f + __expf(-v));
+    case BPDQ_ACT_RELU: return linear_act<BPDQ_ACT_RELU>(v);
+    case BPDQ_ACT_GELU: return linear_act<BPDQ_ACT_GELU>(v);
+    case BPDQ_ACT_GELU_TANH: return linear_act<BPDQ_ACT_GELU_TANH>(v);
+    case BPDQ_ACT_SILU: return linear_act<BPDQ_ACT_SILU>(v);
     default: return v;
   }
 }
@@ -80,6 +102,7 @@ __device__ __forceinline__ u32x4_t linear_load_w(const uint32_t* __restrict__ p,
   return w;
 }
 
+constexpr int kWords = 4;                                 // consecutive words of a lane in the tile kernel
 constexpr int kLinThreads = 512;
 constexpr int kLinWaves = kLinThreads / 64;
 
@@ -148,7 +171,7 @@ __global__ __launch_bounds__(kLinThreads) void linear_rows_kernel(LinearArgs a) 
         const PlaneWord<K> pw(words);
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-          const u32x4_t v = pw.template values<T, false>(levels[r], f);
+          const u32x4_t v = pw.template values<T>(levels[r], f);
 #pragma unroll
           for (int n = 0; n < NT; ++n) acc[r][n] = mfma_16x16x32<T>(v, xs[n][f], acc[r][n]);
         }
@@ -183,42 +206,66 @@ __device__ __forceinline__ f32x16_t mfma_32x32x16(u32x4_t a, u32x4_t b, f32x16_t
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// One LDS-DMA load: 64 lanes x 16 bytes from `base + voff` (per lane) to the 1 KB of LDS that starts at byte address lds_addr
+// (wave-uniform, handed over in M0, which has to be one wait state old when the load reads it: the s_nop).  One outstanding vector-memory
+// operation of the wavefront.
+__device__ __forceinline__ void lds_dma_1k(const void* base, unsigned voff, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+}
+// Waits until at most N vector-memory operations are outstanding (the other counters' fields at their maxima).
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt has six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070 | 0x0f00);
+}
+
 // Shape of a work-group of the tile kernel: WR x WT wavefronts of RT x TT blocks of 32 rows x 32 tokens, KS times over the columns.
-template <int K, int WR_, int WT_, int KS_, int RT_, int TT_>
+template <int K, int WR_, int WT_, int KS_, int RT_, int TT_, int STAGES_>
 struct LinearTile {
-  static constexpr int WR = WR_, WT = WT_, KS = KS_, RT = RT_, TT = TT_;
+  static constexpr int WR = WR_, WT = WT_, KS = KS_, RT = RT_, TT = TT_, kStages = STAGES_;
   static constexpr int kRows = 32 * RT * WR, kToks = 32 * TT * WT;
   static constexpr int kPart = 64 * WR * WT, kThreads = kPart * KS;
-  static constexpr int kWords = K <= 2 ? 4 : 2;          // consecutive words of a lane: fewer where more planes take the registers
-  static constexpr int kPieces = kToks * 8 / kPart;      // 16-byte pieces of X that a thread moves per 64 columns
-  static constexpr int kBuf = kToks * 128;               // bytes of 64 columns of X
-  static constexpr size_t kLds = (size_t)2 * KS * kBuf;
+  static constexpr int kDma = kToks * 128 / 1024 / (WR * WT);       // requests of a wavefront per 64 columns
+  static constexpr int kStage = kToks * 128;             // bytes of 64 columns of X
+  static constexpr int kLevel = 8 * PlaneLevels<_Float16, K>::kRegs;        // bytes of the levels of a row and group
+  static constexpr int kTable = 2 * kRows * kLevel;      // of the rows' levels of a stage, one word for each half
+  static constexpr int kRing = kStages * KS * kStage;
+  static constexpr size_t kLds = (size_t)kRing + 2 * KS * kTable;
+  static_assert(kLds <= 160 * 1024, "one work-group to a CU");
   static_assert(KS == 1 || (size_t)(KS / 2) * kRows * kToks * 4 <= kLds, "the joining of the parts has to fit");
 };
 
-// Eight rows from `first` of one token: bias, activation, residual, one rounding.
+// X in the order of the tile kernel: images of 32 tokens x 64 columns, [token / 32][chunk of 256 columns][j][4 KB], of words j and 4 + j of the
+// chunk (half 0 and 1).  The operand of (token t, half h, step f), 16 bytes, lies at 128 t + 16 ((4 h + f) ^ (t / 2 & 7)): 16 consecutive tokens
+// of a step and half fall into all 64 banks of LDS.  Tokens from n_tok on and columns from d_in on are zero.
+// One wavefront per image.
 template <typename T>
-__device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, int first, f32x4_t v0, f32x4_t v1, bool vec_y,
-                                               bool vec_r) {
+__global__ __launch_bounds__(256) void linear_order_kernel(LinearArgs a, int n_image, int images, u32x4_t* __restrict__ out) {
+  const int id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= n_image) return;
+  const int block = id / images, at = id % images;       // images: of a block of 32 tokens
+  const int half = threadIdx.x & 1, t = (threadIdx.x & 63) >> 1;
+  const int word = at / 4 * 8 + 4 * half + at % 4;
+  const long tok = 32L * block + t;
+  uint32_t raw[16];
+  linear_load_x(static_cast<const T*>(a.x) + (tok < a.n_tok ? tok : 0) * a.ldx + 32L * word,
+                tok < a.n_tok ? a.d_in - 32 * word : 0, a.vec_x, raw);
+  u32x4_t step[4];
+  plane_order(raw, step);
+  u32x4_t* to = out + (long)id * 256 + 8 * t;
+#pragma unroll
+  for (int f = 0; f < 4; ++f) to[(4 * half + f) ^ (t >> 1 & 7)] = step[f];
+}
+
+// Eight rows from `first` of one token: bias, activation, residual, one rounding.
+template <typename T, int ACT>
+__device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, int first, f32x4_t v0, f32x4_t v1,
+                                               const float (&bias)[8], bool vec_y, bool vec_r) {
   typedef T T8 __attribute__((ext_vector_type(8)));
   float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
   const int n = a.d_out - first < 8 ? a.d_out - first : 8;
-  if (a.bias) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) v[i] += (float)static_cast<const T*>(a.bias)[first + i];
-  }
-  if (a.act != BPDQ_ACT_NONE) {
-#pragma unroll 1
-    for (int i = 0; i < 8; i += 2) {                     // (indexed by registers below: two at a time keep the code small)
-      const float p = linear_act(i == 0 ? v[0] : i == 2 ? v[2] : i == 4 ? v[4] : v[6], a.act);
-      const float q = linear_act(i == 0 ? v[1] : i == 2 ? v[3] : i == 4 ? v[5] : v[7], a.act);
-      if (i == 0) { v[0] = p; v[1] = q; }
-      else if (i == 2) { v[2] = p; v[3] = q; }
-      else if (i == 4) { v[4] = p; v[5] = q; }
-      else { v[6] = p; v[7] = q; }
-    }
-  }
+  for (int i = 0; i < 8; ++i) v[i] = linear_act<ACT>(v[i] + bias[i]);
   if (a.residual) {
     const T* r = static_cast<const T*>(a.residual) + tok * a.ldr + first;
     if (vec_r && n == 8) {
@@ -244,9 +291,18 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
   }
 }
 
-template <typename T, int K, typename S>
-__global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles) {
-  constexpr int W = S::kWords, RT = S::RT, TT = S::TT;
+// VEC: the planes go by 16 bytes.
+//
+// Operands.  X comes in the order of linear_order_kernel, straight from memory into a ring of stages in LDS (LDS-DMA: no registers, no
+// instructions but the request); a row's weights for 256 columns are 16 bytes of each plane per lane (half h of a wavefront: words 4 h ..
+// of the chunk) and are decoded in registers, a step of 16 columns ahead of its products.  The levels of the rows' groups are made by
+// all threads for the next chunk and handed over in LDS.  A stage's barrier stands before its last step, when
+// every wavefront has read the stage and the next one has landed.
+// The compiler does not see the LDS-DMA requests (inline assembly), so the vmcnt waits are written by hand: at most the requests of
+// the stages behind the next one may be outstanding.  Loads that the compiler issues meanwhile only make that wait longer.
+template <typename T, int K, typename S, bool VEC>
+__global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const char* __restrict__ images) {
+  constexpr int W = kWords, RT = S::RT, TT = S::TT;
   extern __shared__ uint4 lds_raw[];
   char* lds = reinterpret_cast<char*>(lds_raw);
   const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / S::kPart);
@@ -256,15 +312,23 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int row0 = blockIdx.x / tok_tiles * S::kRows, tok0 = blockIdx.x % tok_tiles * S::kToks;
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32;
   const int grp_step = wpg % 4 == 0 ? 4 : wpg % 2 == 0 ? 2 : 1;     // words after which a lane's group may change
+  const int all_chunks = bpdq_ceil_div(nw, 2 * W);
+  const int n_chunk = bpdq_ceil_div(all_chunks, S::KS);  // of a part, the last one maybe past the end
 
-  // where the thread's pieces of X and the lane's rows lie, as byte offsets from the tile's first token and row
-  const char* x_base = reinterpret_cast<const char*>(a.x) + (long)tok0 * a.ldx * 2;
-  const int piece = tid & 3, unit0 = tid >> 2;           // unit: (token, half)
-  const int x_tok = unit0 >> 1, x_half = unit0 & 1, x_last = a.n_tok - 1 - tok0;
-  const unsigned x_row = (unsigned)a.ldx * 2u;
-  constexpr int kTokStep = S::kPart / 8;                 // tokens between a thread's pieces
-  static_assert(kTokStep % 8 == 0, "a thread's pieces lie alike in LDS");
-  const unsigned x_lds = (unsigned)(x_tok * 128 + ((4 * x_half) ^ (x_tok & 7)) * 16 + piece * 4);
+  // a stage: kToks / 32 images; the wavefront requests kDma runs of 1 KB.  Stages past the end repeat the last one.
+  const int n_image = 4 * all_chunks;
+  const char* x_from = images + (long)(tok0 / 32) * n_image * 4096;
+  auto request = [&](int stage, int ring) {              // of this part: chunk stage / 4, word stage % 4
+    int at = (stage / W * S::KS + part) * W + stage % W;
+    at = at < n_image ? at : n_image - 1;
+#pragma unroll
+    for (int i = 0; i < S::kDma; ++i) {
+      const int run = wave * S::kDma + i;
+      lds_dma_1k(x_from + ((long)(run / 4) * n_image + at) * 4096 + (run % 4) * 1024, 16u * lane,
+                 (unsigned)((part * S::kStages + ring) * S::kStage + run * 1024));
+    }
+  };
+
   const char* w_base[K];
   const char* c_base[K + 1];
 #pragma unroll
@@ -277,66 +341,82 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     const int at = 32 * (RT * wr + r) + low;
     row[r] = row0 + at < a.d_out ? at : a.d_out - 1 - row0;
   }
-
-  u32x4_t xv[S::kPieces];
-  auto load_x = [&](int chunk, int j) {                  // sub-chunk j: word j of each half
-    const int word = 2 * W * chunk + W * x_half + j;
-    const bool on = word < nw;
-    const unsigned col = (unsigned)(on ? word : 0) * 64u + (unsigned)piece * 16u;
-#pragma unroll
-    for (int i = 0; i < S::kPieces; ++i) {
-      const int t = x_tok + i * kTokStep < x_last ? x_tok + i * kTokStep : x_last;
-      const char* p = x_base + ((unsigned)t * x_row + col);
-      u32x4_t v;
-      if (a.vec_x) {
-        v = *reinterpret_cast<const u32x4_t*>(p);
-      } else {
-        const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (uint32_t)s[2 * e] | (uint32_t)s[2 * e + 1] << 16;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) xv[i][e] = on ? v[e] : 0u;
-    }
-  };
-  auto store_x = [&](int buf) {
-    char* at = lds + (part * 2 + buf) * S::kBuf;
-#pragma unroll
-    for (int i = 0; i < S::kPieces; ++i)
-#pragma unroll
-      for (int f = 0; f < 4; ++f)                        // (4 h + f) ^ (t & 7): f changes the two lowest bits of the slot
-        *reinterpret_cast<uint32_t*>(at + (x_lds ^ (unsigned)(f * 16)) + i * (kTokStep * 128)) = xv[i][f];
-  };
   uint32_t w_cur[RT][K][W], w_next[RT][K][W];
-  auto load_w = [&](int chunk, uint32_t (&w)[RT][K][W]) {
+  auto load_w = [&](int chunk) {                         // words past the end: the row's first, under levels of zero
     const int word = 2 * W * chunk + W * half;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int i = 0; i < K; ++i) {
-        const char* p = w_base[i] + (row[r] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u;
-        if (a.vec_w) {                                   // rows of whole lanes
-          typedef uint32_t words __attribute__((ext_vector_type(W)));
-          const words v = *reinterpret_cast<const words*>(p);
+        if constexpr (VEC) {                             // rows are whole lanes
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(w_base[i] + (row[r] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u);
 #pragma unroll
-          for (int j = 0; j < W; ++j) w[r][i][j] = v[j];
+          for (int j = 0; j < W; ++j) w_next[r][i][j] = v[j];
         } else {
 #pragma unroll
-          for (int j = 0; j < W; ++j) w[r][i][j] = word + j < nw ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
+          for (int j = 0; j < W; ++j)
+            w_next[r][i][j] = *reinterpret_cast<const uint32_t*>(
+                w_base[i] + (row[r] * (unsigned)nw + (unsigned)(word + j < nw ? word + j : 0)) * 4u);
         }
       }
   };
-  _Float16 c_next[RT][K + 1];
-  auto load_c = [&](int chunk, int j) {
-    const int word = 2 * W * chunk + W * half + j;
-    const unsigned g = (unsigned)(word < nw ? word : 0) / (unsigned)wpg;
+  auto take_w = [&]() {
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int i = 0; i <= K; ++i) {
-        const _Float16 v = *reinterpret_cast<const _Float16*>(c_base[i] + (row[r] * (unsigned)n_grp + g) * 2u);
-        c_next[r][i] = word < nw ? v : (_Float16)0.f;    // words past the end add nothing
+      for (int i = 0; i < K; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) w_cur[r][i][j] = w_next[r][i][j];
+  };
+
+  // Levels of the stages whose words begin a group: the part's threads make them for all rows, [half][row], from coefficients that
+  // were requested a stage before.
+  char* table = lds + S::kRing + part * 2 * S::kTable;
+  typedef uint32_t Level __attribute__((ext_vector_type(2 * PlaneLevels<T, K>::kRegs)));
+  constexpr int kUnits = 2 * S::kRows / S::kPart;        // (half, row) pairs of a thread
+  _Float16 c_raw[kUnits][K + 1];
+  auto level_word = [&](int stage, int h) { return 2 * W * (stage / W * S::KS + part) + W * h + stage % W; };
+  auto load_levels = [&](int stage) {
+    if (stage % W % grp_step) return;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int id = u * S::kPart + tid, r = id % S::kRows, word = level_word(stage, id / S::kRows);
+      const unsigned g = (unsigned)(word < nw ? word : 0) / (unsigned)wpg;
+      const unsigned at = row0 + r < a.d_out ? r : a.d_out - 1 - row0;
+#pragma unroll
+      for (int i = 0; i <= K; ++i)
+        c_raw[u][i] = *reinterpret_cast<const _Float16*>(c_base[i] + (at * (unsigned)n_grp + g) * 2u);
+    }
+  };
+  auto store_levels = [&](int stage) {
+    if (stage % W % grp_step) return;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int id = u * S::kPart + tid;
+      const bool on = level_word(stage, id / S::kRows) < nw;        // words past the end add nothing
+      PlaneLevels<T, K> made;
+      made.set(c_raw[u]);
+      Level out;
+#pragma unroll
+      for (int n = 0; n < PlaneLevels<T, K>::kRegs; ++n) {
+        out[2 * n] = on ? made.lo[n] : 0u;
+        out[2 * n + 1] = on ? made.hi[n] : 0u;
       }
+      reinterpret_cast<Level*>(table + (stage & 1) * S::kTable)[id] = out;
+    }
+  };
+  PlaneLevels<T, K> levels[RT];
+  auto read_levels = [&](int stage) {
+    if (stage % W % grp_step) return;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const Level in = reinterpret_cast<const Level*>(table + (stage & 1) * S::kTable)[half * S::kRows + 32 * (RT * wr + r) + low];
+#pragma unroll
+      for (int n = 0; n < PlaneLevels<T, K>::kRegs; ++n) {
+        levels[r].lo[n] = in[2 * n];
+        levels[r].hi[n] = in[2 * n + 1];
+      }
+    }
   };
 
   f32x16_t acc[RT][TT];
@@ -346,56 +426,75 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[r][t][e] = 0.f;
-  PlaneLevels<T, K> levels[RT];
+  u32x4_t b[TT], v[2][RT];
+  const char* b_base = lds + part * S::kStages * S::kStage + (32 * TT * wt + low) * 128;
+  const int b_slot = (4 * half) ^ (low >> 1 & 7);
+  auto read_b = [&](int ring, int f, int t) {
+    b[t] = *reinterpret_cast<const u32x4_t*>(b_base + ring * S::kStage + ((b_slot ^ f) * 16) + t * (32 * 128));
+  };
+  auto decode = [&](int j, int f) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      uint32_t words[K];
+#pragma unroll
+      for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][j];
+      v[f & 1][r] = PlaneWord<K>(words).template values<T>(levels[r], f);
+    }
+  };
 
-  const int n_chunk = bpdq_ceil_div(nw, 2 * W * S::KS);  // chunks of a part, the last ones maybe empty
-  load_x(part, 0);
-  load_w(part, w_next);
-  load_c(part, 0);
-  store_x(0);
-  load_x(part, 1);
+#pragma unroll
+  for (int s = 0; s < S::kStages; ++s) request(s, s);
+  load_w(part);
+  load_levels(0);
+  store_levels(0);
+  load_levels(1);
+  take_w();
+  wait_vm<(S::kStages - 1) * S::kDma>();
   __syncthreads();
+  read_levels(0);
+#pragma unroll
+  for (int t = 0; t < TT; ++t) read_b(0, 0, t);
+  decode(0, 0);
+  int ring = 0;                                          // stage % kStages
   for (int n = 0; n < n_chunk; ++n) {
-    const int chunk = n * S::KS + part, chunk1 = chunk + S::KS;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < K; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j) w_cur[r][i][j] = w_next[r][i][j];
-    load_w(chunk1, w_next);
+    const int chunk1 = (n + 1) * S::KS + part;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      store_x((j + 1) & 1);
-      load_x(j + 2 < W ? chunk : chunk1, (j + 2) % W);
-      if (j % grp_step == 0) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) levels[r].set(c_next[r]);
-        if (j + grp_step < W) load_c(chunk, j + grp_step);
-        else load_c(chunk1, 0);
-      }
-      const char* at = lds + (part * 2 + (j & 1)) * S::kBuf;
+      const int stage = n * W + j, ring1 = ring + 1 < S::kStages ? ring + 1 : 0;
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
-        u32x4_t b[TT];
+        if (f == 0 && j == W / 2) load_w(chunk1);
+        if (f == 2) {
+          store_levels(stage + 1);
+          load_levels(stage + 2);
+        }
+        if (f == 3) {
+          wait_vm<(S::kStages - 2) * S::kDma>();
+          __syncthreads();
+          request(stage + S::kStages, ring);
+          if (j + 1 == W) take_w();
+          read_levels(stage + 1);
+        }
+        decode(f < 3 ? j : (j + 1) % W, (f + 1) & 3);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-          const int tok = 32 * (TT * wt + t) + low;
-          b[t] = *reinterpret_cast<const u32x4_t*>(at + tok * 128 + (((4 * half + f) ^ (tok & 7)) * 16));
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[r][t] = mfma_32x32x16<T>(v[f & 1][r], b[t], acc[r][t]);
+          read_b(f < 3 ? ring : ring1, (f + 1) & 3, t);
         }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          uint32_t words[K];
-#pragma unroll
-          for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][j];
-          const u32x4_t v = PlaneWord<K>(words).template values<T, true>(levels[r], f);
-#pragma unroll
-          for (int t = 0; t < TT; ++t) acc[r][t] = mfma_32x32x16<T>(v, b[t], acc[r][t]);
+        for (int t = 0; t < TT; ++t) {                   // RT products, one read, vector instructions beside them
+          __builtin_amdgcn_sched_group_barrier(0x8, RT, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, 4 * RT, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);               // or the loads would sink to where they are needed
       }
-      __syncthreads();
+      ring = ring1;
     }
   }
+  wait_vm<0>();                                          // the last requests have landed before LDS serves the rest
+  __syncthreads();
 
   // the parts' sums meet in LDS, the upper half of the parts added to the lower until one is left
   if constexpr (S::KS > 1) {
@@ -427,41 +526,58 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   }
   // 32 tokens at a time through the wavefront's 8 KB of LDS, so that eight lanes store 128 consecutive bytes of a token; of a block a
   // lane holds rows 8 q + 4 half + i of token low.  (16-byte slot n of a token's 64 rows lies at n ^ (token & 15).)
-  constexpr int kSlots = 8 * RT;
   static_assert(RT == 2 && (size_t)S::WR * S::WT * 32 * 64 * 4 <= S::kLds, "16 slots a token");
-  f32x4_t* mine = reinterpret_cast<f32x4_t*>(lds) + wave * 32 * kSlots;
-  const bool vec_y = a.vec_y, vec_r = a.vec_r;
-#pragma unroll 1
-  for (int t = 0; t < TT; ++t) {
+  f32x4_t* mine = reinterpret_cast<f32x4_t*>(lds) + wave * 32 * 16;
+  const int s2 = 2 * (lane & 7), first = row0 + 64 * wr + 4 * s2;   // the lane's eight rows
+  float bias[8];
 #pragma unroll
-    for (int u = 0; u < TT; ++u) {
-      if (u != t) continue;                              // uniform: acc stays in registers
+  for (int i = 0; i < 8; ++i) bias[i] = a.bias && first + i < a.d_out ? (float)static_cast<const T*>(a.bias)[first + i] : 0.f;
+  auto finish = [&](auto act) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          mine[low * kSlots + ((8 * r + 2 * q + half) ^ (low & 15))] =
-              f32x4_t{acc[r][u][4 * q], acc[r][u][4 * q + 1], acc[r][u][4 * q + 2], acc[r][u][4 * q + 3]};
+          mine[low * 16 + ((8 * r + 2 * q + half) ^ (low & 15))] =
+              f32x4_t{acc[r][t][4 * q], acc[r][t][4 * q + 1], acc[r][t][4 * q + 2], acc[r][t][4 * q + 3]};
+      __builtin_amdgcn_wave_barrier();                   // (LDS serves a wavefront in order)
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int k = it * 8 + (lane >> 3);
+        const f32x4_t v0 = mine[k * 16 + (s2 ^ (k & 15))], v1 = mine[k * 16 + ((s2 + 1) ^ (k & 15))];
+        const long tok = tok0 + 32 * (TT * wt + t) + k;
+        if (tok < a.n_tok && first < a.d_out) linear_finish8<T, act.value>(a, tok, first, v0, v1, bias, a.vec_y, a.vec_r);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();                     // (LDS serves a wavefront in order)
-#pragma unroll 1
-    for (int it = 0; it < 32 * kSlots / 2 / 64; ++it) {
-      const int k = it * 8 + (lane >> 3), s2 = 2 * (lane & 7);
-      const f32x4_t v0 = mine[k * kSlots + (s2 ^ (k & 15))], v1 = mine[k * kSlots + ((s2 + 1) ^ (k & 15))];
-      const long tok = tok0 + 32 * (TT * wt + t) + k;
-      const int first = row0 + 32 * RT * wr + 4 * s2;
-      if (tok < a.n_tok && first < a.d_out) linear_finish8<T>(a, tok, first, v0, v1, vec_y, vec_r);
-    }
-    __builtin_amdgcn_wave_barrier();
+  };
+  switch (a.act) {
+    case BPDQ_ACT_RELU: finish(std::integral_constant<int, BPDQ_ACT_RELU>()); break;
+    case BPDQ_ACT_GELU: finish(std::integral_constant<int, BPDQ_ACT_GELU>()); break;
+    case BPDQ_ACT_GELU_TANH: finish(std::integral_constant<int, BPDQ_ACT_GELU_TANH>()); break;
+    case BPDQ_ACT_SILU: finish(std::integral_constant<int, BPDQ_ACT_SILU>()); break;
+    default: finish(std::integral_constant<int, BPDQ_ACT_NONE>()); break;
   }
 }
 
 template <typename T, int K, typename S>
 static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
-  BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S>>(S::kLds)));
+  const int images = bpdq_ceil_div(a.d_in, 256) * 4, blocks = bpdq_ceil_div(a.n_tok, S::kToks) * (S::kToks / 32);
+  hipLaunchKernelGGL((linear_order_kernel<T>), dim3(bpdq_ceil_div(images * blocks, 4)), dim3(256), 0, stream, a, images * blocks, images,
+                     static_cast<u32x4_t*>(a.ws));
+  BPDQ_LAUNCH_CHECK();
   const int tok_tiles = bpdq_ceil_div(a.n_tok, S::kToks);
-  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S>), dim3(bpdq_ceil_div(a.d_out, S::kRows) * tok_tiles), dim3(S::kThreads), S::kLds,
-                     stream, a, tok_tiles);
+  const dim3 grid(bpdq_ceil_div(a.d_out, S::kRows) * tok_tiles);
+  if (a.vec_w) {
+    BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, true>>(S::kLds)));
+    hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, true>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
+                       static_cast<const char*>(a.ws));
+  } else {
+    BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, false>>(S::kLds)));
+    hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, false>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
+                       static_cast<const char*>(a.ws));
+  }
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
@@ -477,10 +593,9 @@ static int linear_launch(const LinearArgs& a, hipStream_t stream) {
 template <typename T, int K>
 static int linear_pick(const LinearArgs& a, hipStream_t stream) {
   if (a.n_tok <= 16) return linear_launch<T, K, 1, 1>(a, stream);
-  // offsets inside a tile of X are 32 bits
-  if (a.n_tok <= 32 || a.ldx >= 1L << 22) return linear_launch<T, K, 2, 2>(a, stream);
-  if (a.n_tok <= 1024) return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 4, 2, 4>>(a, stream);
-  return linear_launch_tiles<T, K, LinearTile<K, 4, 2, 1, 2, 4>>(a, stream);
+  if (a.n_tok <= kLinRowsMost) return linear_launch<T, K, 2, 2>(a, stream);
+  if (a.n_tok <= 1024) return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 2, 2, 4, 3>>(a, stream);
+  return linear_launch_tiles<T, K, LinearTile<K, 4, 2, 1, 2, 4, 3>>(a, stream);
 }
 
 template <int K>

@@ -3,9 +3,14 @@
 
 using namespace bpdq;
 
+extern "C" size_t bpdq_linear_workspace_bytes(int n_tok, int d_in) {
+  if (n_tok <= kLinRowsMost || d_in <= 0 || d_in % 32) return 0;
+  return bpdq_align_up((size_t)n_tok, kLinTokPad) * bpdq_align_up((size_t)d_in, 256) * 2;
+}
+
 extern "C" int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,
                            const void* X, int n_tok, long ldx, int dtype, const void* bias, int act, const void* residual,
-                           long ldr, void* Y, long ldy, void* stream_) {
+                           long ldr, void* Y, long ldy, void* ws, size_t ws_bytes, void* stream_) {
   if (!planes || (reinterpret_cast<uintptr_t>(planes) & 3)) return -1;
   if (!coefs_h || (reinterpret_cast<uintptr_t>(coefs_h) & 1)) return -2;
   if (d_out <= 0) return -3;
@@ -23,6 +28,9 @@ extern "C" int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int 
   if (residual && ldr < d_out) return -14;
   if (!Y || (reinterpret_cast<uintptr_t>(Y) & 1)) return -15;
   if (ldy < d_out) return -16;
+  const size_t need = bpdq_linear_workspace_bytes(n_tok, d_in);
+  if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))) return -17;
+  if (ws_bytes < need) return -18;
   LinearArgs a;
   a.planes = planes;
   a.coefs = reinterpret_cast<const _Float16*>(coefs_h);
@@ -30,6 +38,7 @@ extern "C" int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int 
   a.bias = bias;
   a.residual = residual;
   a.y = Y;
+  a.ws = ws;
   a.ldx = ldx;
   a.ldr = ldr;
   a.ldy = ldy;

@@ -7,9 +7,7 @@
 // The codes of four columns as bytes come from the plane words by a shift and a mask if the columns are eight apart, so the 32
 // columns of a word are taken in the order
 //   step f = 0..3:  2f, 2f + 8, 2f + 16, 2f + 24, 2f + 1, 2f + 9, 2f + 17, 2f + 25
-// (the contraction does not care), and the other operand is brought into the same order by plane_order().  In pairs, at two
-// more instructions for eight weights, the order of a step is 2f, 2f + 1, 2f + 8, 2f + 9, ...: then the other operand's step is word f of each
-// of the four 16-byte pieces of its 32 values, and these can be moved as they are.
+// (the contraction does not care), and the other operand is brought into the same order by plane_order().
 // Per weight 0.6 to 2 vector instructions for the codes (two planes: their even bits and their odd bits are merged first, whole
 // words at a time) and one for the tables.
 #pragma once
@@ -93,16 +91,11 @@ struct PlaneWord {
     else return first | ((v[1] >> (2 * f)) & (K == 3 ? 0x01010101u : 0x03030303u)) << 2;
   }
   // the eight values of step f
-  template <typename T, bool PAIRS>
+  template <typename T>
   __device__ __forceinline__ u32x4_t values(const PlaneLevels<T, K>& levels, int f) const {
-    uint32_t a, b, c, d, e = codes(even, f), o = codes(odd, f);
-    if constexpr (PAIRS) {
-      const uint32_t low = __builtin_amdgcn_perm(o, e, 0x05010400u);
-      o = __builtin_amdgcn_perm(o, e, 0x07030602u);
-      e = low;
-    }
-    levels.take(e, a, b);
-    levels.take(o, c, d);
+    uint32_t a, b, c, d;
+    levels.take(codes(even, f), a, b);
+    levels.take(codes(odd, f), c, d);
     return u32x4_t{a, b, c, d};
   }
 };

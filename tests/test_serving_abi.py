@@ -18,7 +18,7 @@ def lib():
 
 
 LINEAR = dict(planes=P, coefs=P, d_out=64, d_in=128, bits=2, group=32, X=P, n_tok=3, ldx=128, dtype=1, bias=None, act=0,
-              residual=None, ldr=0, Y=P, ldy=64, stream=None)
+              residual=None, ldr=0, Y=P, ldy=64, ws=None, ws_bytes=0, stream=None)
 
 
 @pytest.mark.parametrize("change,code", [
@@ -27,9 +27,18 @@ LINEAR = dict(planes=P, coefs=P, d_out=64, d_in=128, bits=2, group=32, X=P, n_to
     (dict(group=96), -6), (dict(X=None), -7), (dict(X=P + 1), -7), (dict(n_tok=-1), -8), (dict(ldx=127), -9), (dict(dtype=0), -10),
     (dict(dtype=3), -10), (dict(bias=P + 1), -11), (dict(act=-1), -12), (dict(act=5), -12), (dict(residual=P + 1), -13),
     (dict(residual=P, ldr=63), -14), (dict(Y=None), -15), (dict(Y=P + 1), -15), (dict(ldy=63), -16),
+    (dict(n_tok=1000), -17), (dict(n_tok=1000, ws=P + 16, ws_bytes=1 << 30), -17), (dict(n_tok=1000, ws=P, ws_bytes=1000), -18),
     (dict(n_tok=0, X=None, Y=None), 0)])
 def test_linear_refuses(lib, change, code):
     assert lib.bpdq_linear(*{**LINEAR, **change}.values()) == code
+
+
+def test_linear_workspace(lib):
+    size = lib.bpdq_linear_workspace_bytes
+    assert size(0, 128) == size(1, 128) == size(-1, 128) == size(1000, 100) == size(1000, 0) == 0
+    for n, d in ((33, 32), (1000, 4096), (4096, 18944), (70000, 29568)):
+        assert size(n, d) % 256 == 0 and size(n, d) >= 2 * n * d
+    assert size(1 << 20, 29568) > 1 << 35                # counted in more than 32 bits
 
 
 def _cache(**change):
