@@ -106,91 +106,139 @@ constexpr int kWords = 4;                                 // consecutive words o
 constexpr int kLinThreads = 512;
 constexpr int kLinWaves = kLinThreads / 64;
 
+constexpr int kRowPitch = 512 + 16;                       // bytes of a token's 256 columns in LDS: 16 tokens fall into all 64 banks
+
 template <typename T, int K, int R, int NT>
-__global__ __launch_bounds__(kLinThreads) void linear_rows_kernel(LinearArgs a) {
+__global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear_rows_kernel(LinearArgs a) {
   constexpr int kRows = 16 * R, kToks = 16 * NT;
-  __shared__ float part[kLinWaves][kToks][kRows];
+  constexpr int kStageBytes = kLinWaves * 16 * kRowPitch, kPartBytes = kLinWaves * kToks * kRows * 4;
+  __shared__ uint4 lds_raw[(kStageBytes > kPartBytes ? kStageBytes : kPartBytes) / 16];
   const int tid = threadIdx.x, lane = tid & 63, low = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row0 = blockIdx.x * kRows, tok0 = blockIdx.y * kToks;
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32;
+  const int toks = a.n_tok - tok0 < kToks ? a.n_tok - tok0 : kToks;
+  char* stage = reinterpret_cast<char*>(lds_raw) + wave * 16 * kRowPitch;
 
   f32x4_t acc[R][NT];
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  long row[R];
-  const T* x[NT];
+  // the next row tile's words and first coefficients, requested a tile ahead
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  u32x2_t w_next[K];
+  _Float16 c_next[K + 1];
+  auto row = [&](int r) { return row0 + 16 * r + low < a.d_out ? row0 + 16 * r + low : a.d_out - 1; };
+  auto load_c = [&](int r, int word, _Float16 (&c)[K + 1]) {
+    const _Float16* p = a.coefs + (long)row(r) * n_grp + (word < nw ? word : 0) / wpg;
 #pragma unroll
-  for (int r = 0; r < R; ++r) row[r] = row0 + 16 * r + low < a.d_out ? row0 + 16 * r + low : a.d_out - 1;
+    for (int i = 0; i <= K; ++i) c[i] = p[(long)i * a.d_out * n_grp];
+  };
+  auto load_w = [&](int r, int word) {                   // words past the end: the row's first, under levels of zero
+    const uint32_t* p = a.planes + (long)row(r) * nw;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int t = tok0 + 16 * n + low;
-    x[n] = static_cast<const T*>(a.x) + (t < a.n_tok ? t : a.n_tok - 1) * a.ldx;
-  }
-  for (int w0 = 16 * wave; w0 < nw; w0 += 16 * kLinWaves) {
-    const int word = w0 + 4 * quarter;                   // the lane's words: word .. word + 3
-    const int there = nw - word;
-    u32x4_t w[R][K];
+    for (int i = 0; i < K; ++i, p += (long)a.d_out * nw) {
+      if (a.vec_w) {
+        w_next[i] = *reinterpret_cast<const u32x2_t*>(p + (word < nw ? word : 0));
+      } else {
+        w_next[i][0] = p[word < nw ? word : 0];
+        w_next[i][1] = p[word + 1 < nw ? word + 1 : 0];
+      }
+    }
+    load_c(r, word, c_next);
+  };
+  if (8 * wave < nw) load_w(0, 8 * wave + 2 * quarter);
+  for (int w0 = 8 * wave; w0 < nw; w0 += 8 * kLinWaves) {
+    const int word = w0 + 2 * quarter;                   // the lane's words: word, word + 1
+    // X of 256 columns to operands, 16 tokens at a time by way of LDS: loads of whole lines.  Rows behind the last token keep what LDS
+    // held: their results are dropped.
+    const int at = w0 + (lane >> 2 & 7);                 // word of the lane's 16 bytes
+    u32x4_t xs[NT][2][4];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int n = 0; n < NT; ++n) {
+      u32x4_t v[8];
 #pragma unroll
-      for (int i = 0; i < K; ++i)
-        w[r][i] = linear_load_w(a.planes + ((long)i * a.d_out + row[r]) * nw + (there > 0 ? word : 0), there, a.vec_w);
-    PlaneLevels<T, K> levels[R];
+      for (int i = 0; i < 8; ++i) {
+        if (16 * n + 2 * i >= toks) break;               // uniform
+        const int t = 16 * n + 2 * i + (lane >> 5) < toks ? 16 * n + 2 * i + (lane >> 5) : toks - 1;
+        const T* x = static_cast<const T*>(a.x) + (tok0 + t) * a.ldx + (at < nw ? 8L * (4 * w0 + (lane & 31)) : 0L);
+        if (a.vec_x) {
+          v[i] = *reinterpret_cast<const u32x4_t*>(x);
+        } else {
+          const unsigned short* e = reinterpret_cast<const unsigned short*>(x);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool on = j < there;
-      // a group's first word, or the lane's first (which may lie inside a group)
-      if (j == 0 || wpg % 4 != 0) {
-        const int grp = (on ? word + j : 0) / wpg;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          _Float16 c[K + 1];
-#pragma unroll
-          for (int i = 0; i <= K; ++i) {
-            c[i] = a.coefs[((long)i * a.d_out + row[r]) * n_grp + grp];
-            if (!on) c[i] = (_Float16)0.f;               // words past the end add nothing
-          }
-          levels[r].set(c);
+          for (int q = 0; q < 4; ++q) v[i][q] = (uint32_t)e[2 * q] | (uint32_t)e[2 * q + 1] << 16;
         }
       }
-      u32x4_t xs[NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        uint32_t raw[16];
-        linear_load_x(x[n] + 32L * (on ? word + j : 0), on ? 32 : 0, a.vec_x, raw);
-        plane_order(raw, xs[n]);
+      for (int i = 0; i < 8; ++i) {
+        if (16 * n + 2 * i >= toks) break;
+        if (at >= nw) v[i] = u32x4_t{0, 0, 0, 0};
+        *reinterpret_cast<u32x4_t*>(stage + (2 * i + (lane >> 5)) * kRowPitch + 16 * (lane & 31)) = v[i];
       }
+      __builtin_amdgcn_wave_barrier();                   // (LDS serves a wavefront in order)
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
+      for (int j = 0; j < 2; ++j) {
+        uint32_t raw[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const u32x4_t u = *reinterpret_cast<const u32x4_t*>(stage + low * kRowPitch + 128 * quarter + 64 * j + 16 * q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) raw[4 * q + e] = u[e];
+        }
+        plane_order(raw, xs[n][j]);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      u32x2_t w[K];
+      _Float16 c[K + 1];
+#pragma unroll
+      for (int i = 0; i < K; ++i) w[i] = w_next[i];
+#pragma unroll
+      for (int i = 0; i <= K; ++i) c[i] = word < nw ? c_next[i] : (_Float16)0.f;      // words past the end add nothing
+      if (r + 1 < R) load_w(r + 1, word);
+      else if (w0 + 8 * kLinWaves < nw) load_w(0, word + 8 * kLinWaves);
+      PlaneLevels<T, K> levels;
+      levels.set(c);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (j == 1 && wpg % 2 != 0) {                    // uniform: the second word may be another group's
+          load_c(r, word + 1, c);
+#pragma unroll
+          for (int i = 0; i <= K; ++i) c[i] = word + 1 < nw ? c[i] : (_Float16)0.f;
+          levels.set(c);
+        }
         uint32_t words[K];
 #pragma unroll
-        for (int i = 0; i < K; ++i) words[i] = w[r][i][j];
+        for (int i = 0; i < K; ++i) words[i] = w[i][j];
         const PlaneWord<K> pw(words);
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-          const u32x4_t v = pw.template values<T>(levels[r], f);
+          const u32x4_t v = pw.template values<T>(levels, f);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) acc[r][n] = mfma_16x16x32<T>(v, xs[n][f], acc[r][n]);
+          for (int n = 0; n < NT; ++n) acc[r][n] = mfma_16x16x32<T>(v, xs[n][j][f], acc[r][n]);
         }
       }
     }
   }
+  __syncthreads();
   // acc: row 4 quarter + i of the tile, token low
+  float* part = reinterpret_cast<float*>(lds_raw);       // [wave][token][row]
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      *reinterpret_cast<f32x4_t*>(&part[wave][16 * n + low][16 * r + 4 * quarter]) = acc[r][n];
+      *reinterpret_cast<f32x4_t*>(part + (wave * kToks + 16 * n + low) * kRows + 16 * r + 4 * quarter) = acc[r][n];
   __syncthreads();
   for (int id = tid; id < kRows * kToks; id += kLinThreads) {
     const int r = row0 + id % kRows, t = tok0 + id / kRows;
     if (r >= a.d_out || t >= a.n_tok) continue;
     float v = 0.f;
 #pragma unroll
-    for (int s = 0; s < kLinWaves; ++s) v += part[s][id / kRows][id % kRows];
+    for (int s = 0; s < kLinWaves; ++s) v += part[s * kToks * kRows + id];
     if (a.bias) v += (float)static_cast<const T*>(a.bias)[r];
     v = linear_act(v, a.act);
     if (a.residual) v += (float)static_cast<const T*>(a.residual)[t * a.ldr + r];
@@ -225,12 +273,14 @@ struct LinearTile {
   static constexpr int WR = WR_, WT = WT_, KS = KS_, RT = RT_, TT = TT_, kStages = STAGES_;
   static constexpr int kRows = 32 * RT * WR, kToks = 32 * TT * WT;
   static constexpr int kPart = 64 * WR * WT, kThreads = kPart * KS;
+  static constexpr int kAcc = 16 * RT * TT;              // accumulators of a lane
   static constexpr int kDma = kToks * 128 / 1024 / (WR * WT);       // requests of a wavefront per 64 columns
   static constexpr int kStage = kToks * 128;             // bytes of 64 columns of X
   static constexpr int kLevel = 8 * PlaneLevels<_Float16, K>::kRegs;        // bytes of the levels of a row and group
   static constexpr int kTable = 2 * kRows * kLevel;      // of the rows' levels of a stage, one word for each half
   static constexpr int kRing = kStages * KS * kStage;
   static constexpr size_t kLds = (size_t)kRing + 2 * KS * kTable;
+  static_assert(kDma % 4 == 0, "a quarter with each step");
   static_assert(kLds <= 160 * 1024, "one work-group to a CU");
   static_assert(KS == 1 || (size_t)(KS / 2) * kRows * kToks * 4 <= kLds, "the joining of the parts has to fit");
 };
@@ -291,7 +341,7 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
   }
 }
 
-// VEC: the planes go by 16 bytes.
+// GS: words after which a lane's group may change (of the four that it has of a chunk), VEC: the planes go by 16 bytes.
 //
 // Operands.  X comes in the order of linear_order_kernel, straight from memory into a ring of stages in LDS (LDS-DMA: no registers, no
 // instructions but the request); a row's weights for 256 columns are 16 bytes of each plane per lane (half h of a wavefront: words 4 h ..
@@ -300,7 +350,7 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
 // every wavefront has read the stage and the next one has landed.
 // The compiler does not see the LDS-DMA requests (inline assembly), so the vmcnt waits are written by hand: at most the requests of
 // the stages behind the next one may be outstanding.  Loads that the compiler issues meanwhile only make that wait longer.
-template <typename T, int K, typename S, bool VEC>
+template <typename T, int K, typename S, int GS, bool VEC>
 __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const char* __restrict__ images) {
   constexpr int W = kWords, RT = S::RT, TT = S::TT;
   extern __shared__ uint4 lds_raw[];
@@ -311,22 +361,27 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int wr = wave % S::WR, wt = wave / S::WR;
   const int row0 = blockIdx.x / tok_tiles * S::kRows, tok0 = blockIdx.x % tok_tiles * S::kToks;
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32;
-  const int grp_step = wpg % 4 == 0 ? 4 : wpg % 2 == 0 ? 2 : 1;     // words after which a lane's group may change
   const int all_chunks = bpdq_ceil_div(nw, 2 * W);
   const int n_chunk = bpdq_ceil_div(all_chunks, S::KS);  // of a part, the last one maybe past the end
 
   // a stage: kToks / 32 images; the wavefront requests kDma runs of 1 KB.  Stages past the end repeat the last one.
   const int n_image = 4 * all_chunks;
   const char* x_from = images + (long)(tok0 / 32) * n_image * 4096;
-  auto request = [&](int stage, int ring) {              // of this part: chunk stage / 4, word stage % 4
+  unsigned run_from[S::kDma];                            // of a run, in bytes from x_from (all of a tile within 32 bits)
+#pragma unroll
+  for (int i = 0; i < S::kDma; ++i) {
+    const int run = wave * S::kDma + i;
+    run_from[i] = (unsigned)(run / 4) * (unsigned)n_image * 4096u + (unsigned)(run % 4) * 1024u;
+  }
+  // A quarter of a stage's runs: requests in one burst hold the wavefront up.  (Two stages leave no time for that.)  Stage of this part: chunk stage / 4, word stage % 4.
+  constexpr bool kBurst = S::kStages == 2;
+  auto request = [&](int stage, int ring, int quarter) {
     int at = (stage / W * S::KS + part) * W + stage % W;
     at = at < n_image ? at : n_image - 1;
+    const unsigned voff = (unsigned)at * 4096u + 16u * lane;
 #pragma unroll
-    for (int i = 0; i < S::kDma; ++i) {
-      const int run = wave * S::kDma + i;
-      lds_dma_1k(x_from + ((long)(run / 4) * n_image + at) * 4096 + (run % 4) * 1024, 16u * lane,
-                 (unsigned)((part * S::kStages + ring) * S::kStage + run * 1024));
-    }
+    for (int i = quarter * (S::kDma / 4); i < (quarter + 1) * (S::kDma / 4); ++i)
+      lds_dma_1k(x_from, voff + run_from[i], (unsigned)((part * S::kStages + ring) * S::kStage + (wave * S::kDma + i) * 1024));
   };
 
   const char* w_base[K];
@@ -370,14 +425,13 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   };
 
   // Levels of the stages whose words begin a group: the part's threads make them for all rows, [half][row], from coefficients that
-  // were requested a stage before.
+  // were requested when the levels before them were made.
   char* table = lds + S::kRing + part * 2 * S::kTable;
   typedef uint32_t Level __attribute__((ext_vector_type(2 * PlaneLevels<T, K>::kRegs)));
   constexpr int kUnits = 2 * S::kRows / S::kPart;        // (half, row) pairs of a thread
   _Float16 c_raw[kUnits][K + 1];
   auto level_word = [&](int stage, int h) { return 2 * W * (stage / W * S::KS + part) + W * h + stage % W; };
   auto load_levels = [&](int stage) {
-    if (stage % W % grp_step) return;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int id = u * S::kPart + tid, r = id % S::kRows, word = level_word(stage, id / S::kRows);
@@ -389,7 +443,6 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     }
   };
   auto store_levels = [&](int stage) {
-    if (stage % W % grp_step) return;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const int id = u * S::kPart + tid;
@@ -407,7 +460,6 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   };
   PlaneLevels<T, K> levels[RT];
   auto read_levels = [&](int stage) {
-    if (stage % W % grp_step) return;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const Level in = reinterpret_cast<const Level*>(table + (stage & 1) * S::kTable)[half * S::kRows + 32 * (RT * wr + r) + low];
@@ -443,13 +495,16 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   };
 
 #pragma unroll
-  for (int s = 0; s < S::kStages; ++s) request(s, s);
+  for (int s = 0; s < S::kStages; ++s)
+#pragma unroll
+    for (int q = 0; q < (kBurst || s < S::kStages - 1 ? 4 : 1); ++q) request(s, s, q);
   load_w(part);
   load_levels(0);
   store_levels(0);
-  load_levels(1);
+  load_levels(GS);
   take_w();
-  wait_vm<(S::kStages - 1) * S::kDma>();
+  if (S::kAcc <= 64) load_w(part + S::KS);
+  wait_vm<(S::kStages - 2) * S::kDma + (kBurst ? S::kDma : S::kDma / 4)>();
   __syncthreads();
   read_levels(0);
 #pragma unroll
@@ -463,17 +518,23 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       const int stage = n * W + j, ring1 = ring + 1 < S::kStages ? ring + 1 : 0;
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
-        if (f == 0 && j == W / 2) load_w(chunk1);
-        if (f == 2) {
-          store_levels(stage + 1);
-          load_levels(stage + 2);
-        }
         if (f == 3) {
+          // A wait of the compiler's for its loads is one for the requests behind them too, and ours for requests is one for its loads
+          // before them: what they bring is taken before the next requests, and they are issued right before these.
+          if (j + 1 == W) take_w();
+          if ((j + 1) % GS == 0) store_levels(stage + 1);
           wait_vm<(S::kStages - 2) * S::kDma>();
           __syncthreads();
-          request(stage + S::kStages, ring);
-          if (j + 1 == W) take_w();
-          read_levels(stage + 1);
+          if (j == (S::kAcc <= 64 ? W - 1 : W / 2 - 1)) load_w(S::kAcc <= 64 ? chunk1 + S::KS : chunk1);
+          if ((j + 1) % GS == 0) load_levels(stage + 1 + GS);
+          if ((j + 1) % GS == 0) read_levels(stage + 1);
+        }
+        // the slot of the stage before is free behind its barrier
+        if (f == 3) {
+#pragma unroll
+          for (int q = 0; q < (kBurst ? 4 : 1); ++q) request(stage + S::kStages, ring, q);
+        } else if (!kBurst) {
+          request(stage + S::kStages - 1, ring > 0 ? ring - 1 : S::kStages - 1, f + 1);
         }
         decode(f < 3 ? j : (j + 1) % W, (f + 1) & 3);
 #pragma unroll
@@ -532,33 +593,46 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   float bias[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) bias[i] = a.bias && first + i < a.d_out ? (float)static_cast<const T*>(a.bias)[first + i] : 0.f;
-  auto finish = [&](auto act) {
+  auto finish = [&](int t, auto act) {
+#pragma unroll 1
+    for (int it = 0; it < 4; ++it) {
+      const int k = it * 8 + (lane >> 3);
+      const f32x4_t v0 = mine[k * 16 + (s2 ^ (k & 15))], v1 = mine[k * 16 + ((s2 + 1) ^ (k & 15))];
+      const long tok = tok0 + 32 * (TT * wt + t) + k;
+      if (tok < a.n_tok && first < a.d_out) linear_finish8<T, act.value>(a, tok, first, v0, v1, bias, a.vec_y, a.vec_r);
+    }
+  };
+#pragma unroll 1
+  for (int t = 0; t < TT; ++t) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
+    for (int u = 0; u < TT; ++u) {
+      if (u != t) continue;                              // uniform: acc stays in registers
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           mine[low * 16 + ((8 * r + 2 * q + half) ^ (low & 15))] =
-              f32x4_t{acc[r][t][4 * q], acc[r][t][4 * q + 1], acc[r][t][4 * q + 2], acc[r][t][4 * q + 3]};
-      __builtin_amdgcn_wave_barrier();                   // (LDS serves a wavefront in order)
-#pragma unroll
-      for (int it = 0; it < 4; ++it) {
-        const int k = it * 8 + (lane >> 3);
-        const f32x4_t v0 = mine[k * 16 + (s2 ^ (k & 15))], v1 = mine[k * 16 + ((s2 + 1) ^ (k & 15))];
-        const long tok = tok0 + 32 * (TT * wt + t) + k;
-        if (tok < a.n_tok && first < a.d_out) linear_finish8<T, act.value>(a, tok, first, v0, v1, bias, a.vec_y, a.vec_r);
-      }
-      __builtin_amdgcn_wave_barrier();
+              f32x4_t{acc[r][u][4 * q], acc[r][u][4 * q + 1], acc[r][u][4 * q + 2], acc[r][u][4 * q + 3]};
     }
-  };
-  switch (a.act) {
-    case BPDQ_ACT_RELU: finish(std::integral_constant<int, BPDQ_ACT_RELU>()); break;
-    case BPDQ_ACT_GELU: finish(std::integral_constant<int, BPDQ_ACT_GELU>()); break;
-    case BPDQ_ACT_GELU_TANH: finish(std::integral_constant<int, BPDQ_ACT_GELU_TANH>()); break;
-    case BPDQ_ACT_SILU: finish(std::integral_constant<int, BPDQ_ACT_SILU>()); break;
-    default: finish(std::integral_constant<int, BPDQ_ACT_NONE>()); break;
+    __builtin_amdgcn_wave_barrier();                     // (LDS serves a wavefront in order)
+    switch (a.act) {
+      case BPDQ_ACT_RELU: finish(t, std::integral_constant<int, BPDQ_ACT_RELU>()); break;
+      case BPDQ_ACT_GELU: finish(t, std::integral_constant<int, BPDQ_ACT_GELU>()); break;
+      case BPDQ_ACT_GELU_TANH: finish(t, std::integral_constant<int, BPDQ_ACT_GELU_TANH>()); break;
+      case BPDQ_ACT_SILU: finish(t, std::integral_constant<int, BPDQ_ACT_SILU>()); break;
+      default: finish(t, std::integral_constant<int, BPDQ_ACT_NONE>()); break;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <typename T, int K, typename S, int GS, bool VEC>
+static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, hipStream_t stream) {
+  BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, GS, VEC>>(S::kLds)));
+  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, GS, VEC>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
+                     static_cast<const char*>(a.ws));
+  BPDQ_LAUNCH_CHECK();
+  return 0;
 }
 
 template <typename T, int K, typename S>
@@ -569,17 +643,13 @@ static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
   BPDQ_LAUNCH_CHECK();
   const int tok_tiles = bpdq_ceil_div(a.n_tok, S::kToks);
   const dim3 grid(bpdq_ceil_div(a.d_out, S::kRows) * tok_tiles);
+  const int wpg = a.group / 32;
   if (a.vec_w) {
-    BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, true>>(S::kLds)));
-    hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, true>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
-                       static_cast<const char*>(a.ws));
-  } else {
-    BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, false>>(S::kLds)));
-    hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, false>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
-                       static_cast<const char*>(a.ws));
+    if (wpg % 4 == 0) return linear_launch_as<T, K, S, 4, true>(a, grid, tok_tiles, stream);
+    if (wpg % 2 == 0) return linear_launch_as<T, K, S, 2, true>(a, grid, tok_tiles, stream);
+    return linear_launch_as<T, K, S, 1, true>(a, grid, tok_tiles, stream);
   }
-  BPDQ_LAUNCH_CHECK();
-  return 0;
+  return linear_launch_as<T, K, S, 1, false>(a, grid, tok_tiles, stream);
 }
 
 template <typename T, int K, int R, int NT>
@@ -590,12 +660,66 @@ static int linear_launch(const LinearArgs& a, hipStream_t stream) {
   return 0;
 }
 
+// The kernel of a call: the one whose estimate is the least.  A work-group takes a CU, so the time is the rounds of 256 of them times a
+// work-group's, which was measured alone on the chip (two planes, us):
+//   few tokens (R row tiles, 16 or 32 tokens), per 3584 columns: 5.4 + 1.6 R, 8 + 2.2 R
+//   tiles, per 64 columns: 256 x 256 1.25, 256 x 128 0.9, 128 x 128 in two parts 1.15 / 2, 128 x 64 in four 1.85 / 4; 8 for the order of X
+// 64 x 8192 -> 8192: R = 5, 2 x 16 tokens 40 us, tiles of 128 x 64 64, of 256 x 256 193; 2048 x 8192 -> 8192: 256 x 256 294, 128 x 64 535;
+// 333 x 3584 -> 18944: 256 x 128 61, 128 x 128 80, 256 x 256 86.
+enum LinearKernel { kRows1, kRows2, kTile256, kTile256x128, kTile128, kTile128x64 };
+struct LinearPlan {
+  int kernel, r;
+};
+static inline LinearPlan linear_plan(int n_tok, int d_in, int d_out, long ldx) {
+  LinearPlan best = {kRows1, 1};
+  float least = 0.f;
+  auto offer = [&](int kernel, int r, int rows, int toks, float each, float once) {
+    const long groups = ((long)d_out + rows - 1) / rows * (((long)n_tok + toks - 1) / toks);
+    const float t = (float)((groups + 255) / 256) * each + once;
+    if (least == 0.f || t < least) {
+      least = t;
+      best = {kernel, r};
+    }
+  };
+  const float wide = d_in / 3584.f;
+  for (int r : {1, 2, 3, 5, 8}) {
+    offer(kRows1, r, 16 * r, 16, (5.4f + 1.6f * r) * wide, 0.f);
+    if (n_tok > 16 && r > 1 && r < 8) offer(kRows2, r, 16 * r, 32, (8.f + 2.2f * r) * wide, 0.f);
+  }
+  // offsets inside a row tile's planes, inside a token tile of the ordered X and so on are 32 bits in the tile kernels
+  if (n_tok > kLinRowsMost && d_in <= 1 << 20 && ldx > 0) {
+    const float stages = 4.f * bpdq_ceil_div(d_in, 256);
+    offer(kTile256, 0, 256, 256, 1.25f * stages, 8.f);
+    offer(kTile256x128, 0, 256, 128, 0.9f * stages, 8.f);
+    offer(kTile128, 0, 128, 128, 1.15f / 2 * stages, 8.f);
+    offer(kTile128x64, 0, 128, 64, 1.85f / 4 * stages, 8.f);
+  }
+  return best;
+}
+
+template <typename T, int K, int NT>
+static int linear_launch_rows(const LinearArgs& a, int r, hipStream_t stream) {
+  if (r == 2) return linear_launch<T, K, 2, NT>(a, stream);
+  if (r == 3) return linear_launch<T, K, 3, NT>(a, stream);
+  if (r == 5) return linear_launch<T, K, 5, NT>(a, stream);
+  if constexpr (NT == 1) {
+    if (r == 8) return linear_launch<T, K, 8, NT>(a, stream);
+    return linear_launch<T, K, 1, NT>(a, stream);
+  }
+  return BPDQ_ERR_LAUNCH;                                // not offered
+}
+
 template <typename T, int K>
 static int linear_pick(const LinearArgs& a, hipStream_t stream) {
-  if (a.n_tok <= 16) return linear_launch<T, K, 1, 1>(a, stream);
-  if (a.n_tok <= kLinRowsMost) return linear_launch<T, K, 2, 2>(a, stream);
-  if (a.n_tok <= 1024) return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 2, 2, 4, 3>>(a, stream);
-  return linear_launch_tiles<T, K, LinearTile<K, 4, 2, 1, 2, 4, 3>>(a, stream);
+  const LinearPlan p = linear_plan(a.n_tok, a.d_in, a.d_out, a.ldx);
+  switch (p.kernel) {
+    case kRows1: return linear_launch_rows<T, K, 1>(a, p.r, stream);
+    case kRows2: return linear_launch_rows<T, K, 2>(a, p.r, stream);
+    case kTile256: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 8, 3>>(a, stream);
+    case kTile256x128: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 4, 3>>(a, stream);
+    case kTile128: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 2, 2, 4, 3>>(a, stream);
+    default: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 4, 2, 2, 3>>(a, stream);
+  }
 }
 
 template <int K>
