@@ -20,9 +20,11 @@
 namespace bpdq {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / 64;
+constexpr int kAttnMostChunks = 512;                     // of a work item
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnArgs {
@@ -37,6 +39,7 @@ struct AttnArgs {
   long ldq, ldo;
   int max_pages, n_tok, max_q, max_kv, n_q, group;
   int causal, window;
+  int vec_q, vec_o;                                      // whether Q goes by 16 bytes, and out by four values
   int q_tiles, n_chunk, chunk_tiles;
   float scale;
 };
@@ -95,6 +98,18 @@ __device__ __forceinline__ f16x8_t attn_codes(uint32_t a, uint32_t b) {
   return out;
 }
 
+template <typename T>
+__device__ __forceinline__ void attn_store4(T* to, f32x4_t v, bool vec) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  const T4 out = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+  if (vec) {
+    *reinterpret_cast<T4*>(to) = out;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = out[e];
+  }
+}
+
 // T: type of Q and out;  D: head dimension;  NQ: tiles of 16 rows.
 template <typename T, int D, int NQ>
 __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
@@ -106,6 +121,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
   const int chunk = blockIdx.x % a.n_chunk;
   const int item = blockIdx.x / a.n_chunk;               // (head, query tile)
   const int h = item % a.c.n_kv, q_tile = item / a.c.n_kv, seq = blockIdx.y;
+  const int per_page = a.c.page / kKvTile;
   const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
   if (!it.there) return;                                 // uniform
   const int n_chunk = attn_chunks(it, a.chunk_tiles);
@@ -124,14 +140,22 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
     const int i = (on ? r : 0) / a.group, head = h * a.group + (on ? r : 0) % a.group;
     const T* q = static_cast<const T*>(a.q) + (long)(it.first + i) * a.ldq + (long)head * D;
     float most = 0.f;
-    T x[C][16];
+    alignas(16) T x[C][16];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const T* from = q + 64 * c + 16 * quarter;
+      if (a.vec_q) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) reinterpret_cast<u32x4_t*>(x[c])[e] = reinterpret_cast<const u32x4_t*>(from)[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[c][e] = from[e];
+      }
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[c][e] = q[64 * c + 16 * quarter + e];
-        most = fmaxf(most, fabsf((float)x[c][e]));
-      }
+      for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf((float)x[c][e]));
     float f = 1.f, back = 1.f;
     if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
       most = fmaxf(most, __shfl_xor(most, 16, 64));
@@ -163,16 +187,38 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const int per_page = a.c.page / kKvTile;
-  for (int tile = t_begin + wave; tile < t_end; tile += kAttnWaves) {
-    const int page = tile / per_page;
-    const int id = a.table[(long)seq * a.max_pages + page];
-    if (id < 0 || id >= a.c.n_pages) continue;           // uniform
-    const long at = (long)id * a.c.n_kv + h;
-    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(a.c.k + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
-    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(a.c.v + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
-    const float k_scale = a.c.k_scale[at];
-    float v_scale = a.c.v_scale[at];
+  // A tile's K is requested while the tile before is worked on, its V before its own scores: some 8 KB of a wavefront are always on
+  // their way.  Pages outside the cache are stepped over.
+  const int* row_of_table = a.table + (long)seq * a.max_pages;
+  auto page_from = [&](int& tile) {                      // of the next tile from `tile` on that is there, or -1
+    for (; tile < t_end; tile += kAttnWaves) {
+      const int id = row_of_table[tile / per_page];
+      if (id >= 0 && id < a.c.n_pages) return id;
+    }
+    return -1;
+  };
+  u32x4_t kw[4 * C], vw[DT];
+  long at = 0;                                           // page and head
+  float k_scale = 0.f, v_scale = 0.f;
+  auto load_k = [&](int id, int tile) {
+    at = (long)id * a.c.n_kv + h;
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.k + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+#pragma unroll
+    for (int n = 0; n < 4 * C; ++n) kw[n] = from[n * 64];
+  };
+  int tile = t_begin + wave;
+  int id = page_from(tile);
+  if (id >= 0) load_k(id, tile);
+  while (id >= 0) {
+    {
+      const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.v + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vw[d] = from[d * 64];
+    }
+    k_scale = a.c.k_scale[at];
+    v_scale = a.c.v_scale[at];
+    int tile_next = tile + kAttnWaves;
+    const int id_next = page_from(tile_next);
     f32x4_t s[NQ][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -180,7 +226,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
       for (int n = 0; n < NQ; ++n) s[n][u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const u32x4_t w = kp[(u * C + c) * 64];
+        const u32x4_t w = kw[u * C + c];
         const f16x8_t k0 = attn_codes(w[0], w[1]), k1 = attn_codes(w[2], w[3]);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -189,6 +235,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
         }
       }
     }
+    if (id_next >= 0) load_k(id_next, tile_next);
     // values of a page whose scale is not finite reach the rows that see them, and no others: by the probabilities
     const bool bad = !(fabsf(v_scale) < __builtin_huge_valf());
     if (bad) v_scale = 1.f;
@@ -227,7 +274,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
     }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      const u32x4_t w = vp[d * 64];
+      const u32x4_t w = vw[d];
       const f16x8_t v0 = attn_codes(w[0], w[1]), v1 = attn_codes(w[2], w[3]);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
@@ -238,6 +285,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
         for (int i = 0; i < 4; ++i) o[n][d][i] = fmaf(o[n][d][i], fade[n], v_scale * pv[i]);
       }
     }
+    tile = tile_next;
+    id = id_next;
   }
 
   // join the wavefronts
@@ -299,51 +348,367 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
       const int i = (it.r0 + r) / a.group, head = h * a.group + (it.r0 + r) % a.group;
       T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D + d;
       const float f = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) to[e] = (T)(v[e] * f);
+      attn_store4(to, v * f, a.vec_o);
       if (a.lse && d == 0)
         a.lse[(long)(it.first + i) * a.n_q + head] = sum == 0.f ? -__builtin_huge_valf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
   }
 }
 
-// Joins the chunks of a work item, in order.
-template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
-  const int h = blockIdx.x % a.c.n_kv, q_tile = blockIdx.x / a.c.n_kv, seq = blockIdx.y;
+// Many rows (prompts): products of 32 x 32, and K and V of a tile turned into fp16 once for the work-group's 128 rows, in LDS, in operand
+// order.  A wavefront owns 32 rows; S^T = K Q^T and O^T = V^T P^T as above (row a of the first product's operand is the token that makes a lane's
+// scores the second one's operand: 16 s + 8 j + 4 h + i <-> token 16 s + 8 h + 4 j + i of 32).
+//
+// What bounds it is the vector unit, so the softmax is kept to a multiply-add, an exponential, a maximum, a sum and half a conversion per score:
+//  - the running maximum is followed lazily: sums are rescaled only when a row's scores grow by more than 2^8, so probabilities are up to 2^8
+//    relative to the reference and are held as 2^7 times that (fp16 reaches 2^16; what lies below 2^-21 of the reference becomes denormal);
+//  - the scale of V goes into the exponent, relative to a reference v_ref that changes when it is exceeded or undershot by 2^10, so P V adds up
+//    in the accumulators; the row's sum takes it out again, once per tile.
+// The scale of scores must not be negative for the maximum: its sign goes into Q.
+template <typename T, int D>
+struct AttnPrompt {
+  static constexpr int kRows = 128, kKs = D / 16, kDt = D / 32;
+  static constexpr int kBuf = 2 * kKvTile * D * 2;       // bytes of a tile's K and V as fp16
+  static constexpr int kChunks = kKvTile * D / 16 / kAttnThreads;   // 16-byte chunks of K, and of V, of a thread
+  static constexpr size_t kLds = 2 * kBuf;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_kernel(AttnArgs a) {
+  typedef AttnPrompt<T, D> P;
+  constexpr int ROWS = P::kRows, kKs = P::kKs, kDt = P::kDt, kChunks = P::kChunks;
+  extern __shared__ uint4 lds_raw[];
+  char* lds = reinterpret_cast<char*>(lds_raw);
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int chunk = blockIdx.x % a.n_chunk;
+  const int item = blockIdx.x / a.n_chunk;
+  // the last queries see most: they go first
+  const int h = item % a.c.n_kv, q_tile = a.q_tiles - 1 - item / a.c.n_kv, seq = blockIdx.y;
+  const int per_page = a.c.page / kKvTile;
   const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
-  if (!it.there) return;
+  if (!it.there) return;                                 // uniform
   const int n_chunk = attn_chunks(it, a.chunk_tiles);
-  if (n_chunk <= 1) return;                              // written by the first launch
-  const int out_rows = it.rows - it.r0 < ROWS ? it.rows - it.r0 : ROWS;
-  const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk;
-  const long n_slot = (long)gridDim.y * a.q_tiles * a.c.n_kv * a.n_chunk;
-  const float* ml = a.part + n_slot * ROWS * D + slot * ROWS * 2;
-  for (int id = threadIdx.x + blockIdx.z * kAttnThreads; id < out_rows * (D / 4); id += kAttnThreads * gridDim.z) {
-    const int r = id / (D / 4), d = 4 * (id % (D / 4));
-    float top = -__builtin_huge_valf();
-    for (int c = 0; c < n_chunk; ++c) top = fmaxf(top, ml[((long)c * ROWS + r) * 2]);
-    float sum = 0.f;
-    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < n_chunk; ++c) {
-      const float mc = ml[((long)c * ROWS + r) * 2], lc = ml[((long)c * ROWS + r) * 2 + 1];
-      const float f = mc == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(mc - top);
-      sum = fmaf(lc, f, sum);
-      const f32x4_t part = *reinterpret_cast<const f32x4_t*>(a.part + ((slot + c) * ROWS + r) * D + d);
+  if (chunk >= n_chunk) return;
+  const int t_begin = it.tile_lo + chunk * a.chunk_tiles;
+  const int t_end = it.tile_hi < t_begin + a.chunk_tiles ? it.tile_hi : t_begin + a.chunk_tiles;
+
+  // the wavefront's rows: operands, and what they see
+  const int r = it.r0 + 32 * wave + col;
+  const bool on = r < it.rows;
+  const int i = (on ? r : 0) / a.group, head = h * a.group + (on ? r : 0) % a.group;
+  f16x8_t qf[kKs];
+  float q_scale;
+  {
+    const T* q = static_cast<const T*>(a.q) + (long)(it.first + i) * a.ldq + (long)head * D + 8 * half;
+    alignas(16) T x[kKs][8];
+    float most = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(part[e], f, v[e]);
+    for (int k = 0; k < kKs; ++k) {
+      if (a.vec_q) {
+        *reinterpret_cast<u32x4_t*>(x[k]) = *reinterpret_cast<const u32x4_t*>(q + 16 * k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[k][e] = q[16 * k + e];
+      }
     }
-    const int i = (it.r0 + r) / a.group, head = h * a.group + (it.r0 + r) % a.group;
-    T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D + d;
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) to[e] = (T)(v[e] * f);
-    if (a.lse && d == 0)
-      a.lse[(long)(it.first + i) * a.n_q + head] = sum == 0.f ? -__builtin_huge_valf() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int k = 0; k < kKs; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)x[k][e]));
+    float f = a.scale < 0.f ? -1.f : 1.f, back = 1.f;
+    if constexpr (!__is_same(T, _Float16)) {
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      if (most > 0.f && most < __builtin_huge_valf()) {  // into [2^14, 2^15)
+        int e;
+        (void)frexpf(most, &e);
+        e = 15 - e < 126 ? 15 - e : 126;
+        f *= ldexpf(1.f, e);
+        back = ldexpf(1.f, -e);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kKs; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[k][e] = (_Float16)((float)x[k][e] * f);
+    q_scale = back * (fabsf(a.scale) * kLog2e);
+  }
+  const int at_q = it.kv - it.q_len + i;
+  const int see_lo = a.window > 0 ? at_q - a.window + 1 : 0;
+  const int see_hi = !on ? 0 : a.causal && at_q + 1 < it.kv ? at_q + 1 : it.kv;
+  // of all the wavefront's rows: tokens that some see, and that all see
+  int any_lo = on ? see_lo : 0x7fffffff, any_hi = see_hi, all_lo = on ? see_lo : 0, all_hi = on ? see_hi : 0x7fffffff;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const int a0 = __shfl_xor(any_lo, o, 64), a1 = __shfl_xor(any_hi, o, 64), a2 = __shfl_xor(all_lo, o, 64), a3 = __shfl_xor(all_hi, o, 64);
+    any_lo = any_lo < a0 ? any_lo : a0;
+    any_hi = any_hi > a1 ? any_hi : a1;
+    all_lo = all_lo > a2 ? all_lo : a2;
+    all_hi = all_hi < a3 ? all_hi : a3;
+  }
+  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+  any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+  // The thread's chunks of a tile, and where they lie in LDS.  K: of 32 rows and 16 channels, [32 tokens][16 channels][half][row]; V: of 16
+  // tokens and 32 channels, [16 tokens][32 channels][half][channel].
+  u32x4_t kw[kChunks], vw[kChunks];
+  float k_scale = 0.f, v_scale = 0.f, k_scale_next = 0.f, v_scale_next = 0.f;
+  bool there = false, there_next = false;
+  const int* row_of_table = a.table + (long)seq * a.max_pages;
+  auto load = [&](int tile) {                            // a page outside the cache: another one's data, not looked at
+    const int id = tile < t_end ? row_of_table[tile / per_page] : -1;
+    there_next = id >= 0 && id < a.c.n_pages;
+    if (!there_next) return;                             // uniform
+    const long at = (long)id * a.c.n_kv + h;
+    const long byte = at * a.c.page * D + (long)(tile % per_page) * kKvTile * D;
+    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(a.c.k + byte);
+    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(a.c.v + byte);
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n) {
+      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;       // u: (32 tokens, 16 channels) or (16 tokens, 32 channels)
+      const int ut = u / kKs, ks = u % kKs;
+      const int jr = rr & 3, hh = rr >> 2 & 1, jq = rr >> 3 & 1, sl = rr >> 4;
+      kw[n] = kp[((2 * hh + jq) * kKs + ks) * 16 + 4 * (2 * ut + sl) + jr];
+      const int s = u % 4, dt = u / 4;
+      vw[n] = vp[((2 * dt + (rr >> 4)) * 4 + s) * 16 + (rr & 15)];
+    }
+    k_scale_next = a.c.k_scale[at];
+    const float scale = a.c.v_scale[at];
+    v_scale_next = scale < 0x1p-120f ? 0x1p-120f : scale;         // (of zeros; the exponent wants a logarithm)
+  };
+  auto store = [&](int buf) {
+    char* to = lds + buf * P::kBuf;
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n) {
+      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;
+      f16x8_t* k = reinterpret_cast<f16x8_t*>(to + u * 1024) + rr;
+      k[0] = attn_codes(kw[n][0], kw[n][1]);
+      k[32] = attn_codes(kw[n][2], kw[n][3]);
+      f16x8_t* v = reinterpret_cast<f16x8_t*>(to + kKvTile * D * 2 + ((u % 4) * kDt + u / 4) * 1024) + rr;
+      v[0] = attn_codes(vw[n][0], vw[n][1]);
+      v[32] = attn_codes(vw[n][2], vw[n][3]);
+    }
+  };
+
+  f32x16_t o[kDt];
+#pragma unroll
+  for (int d = 0; d < kDt; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  float m = -__builtin_huge_valf(), l = 0.f;             // reference and sum of the lane's row (half of its tokens)
+  float v_ref = 0.f;
+  if (t_begin < t_end) {
+    load(t_begin);
+    if (there_next) store(0);
+  }
+  there = there_next;
+  k_scale = k_scale_next;
+  v_scale = v_scale_next;
+  load(t_begin + 1);
+  __syncthreads();
+  for (int tile = t_begin; tile < t_end; ++tile) {
+    const int buf = (tile - t_begin) & 1, t0 = tile * kKvTile;
+    const char* kl = lds + buf * P::kBuf + 16 * lane;
+    const char* vl = kl + kKvTile * D * 2;
+    const bool work = there && t0 < any_hi && t0 + kKvTile > any_lo;      // uniform
+    f32x16_t s[2];
+    if (work) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < kKs; ++k)
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8_t*>(kl + (u * kKs + k) * 1024), qf[k], s[u], 0, 0, 0);
+      }
+    }
+    if (there_next) store(buf ^ 1);
+    const bool there_after = there_next;
+    const float k_after = k_scale_next, v_after = v_scale_next;
+    load(tile + 2);
+    if (work) {
+      // scores of register e of half u: token t0 + 32 u + 16 (e / 8) + 8 half + e % 8
+      const bool mask = t0 < all_lo || t0 + kKvTile > all_hi;
+      const float f = k_scale * q_scale;
+      float top = -3.0e38f;
+      if (mask) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int t = t0 + 32 * u + 16 * (e / 8) + 8 * half + e % 8;
+            top = fmaxf(top, t >= see_lo && t < see_hi ? s[u][e] : -3.0e38f);
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
+      if (__any(top > m + 8.f)) {
+        const float m_new = fmaxf(m, top);
+        const float fade = m_new == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= fade;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= fade;
+      }
+      // (a scale of V that is not finite fails both comparisons, and then reaches the rows that see the tile through the exponent)
+      float ratio = v_scale / v_ref;
+      if (!(ratio <= 1.f && ratio >= 0x1p-10f)) {
+        // 2^64 bounds the sums: what was added under a scale that much larger stays what counts
+        const float ref = 2.f * v_scale;
+        const float by = v_ref / ref;
+        if (v_scale < __builtin_huge_valf() && by < 0x1p64f) {
+#pragma unroll
+          for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] *= by;
+          v_ref = ref;
+        }
+        ratio = v_scale / v_ref;
+      }
+      const float shift = v_scale < __builtin_huge_valf() ? 7.f + __builtin_amdgcn_logf(ratio) : __builtin_nanf("");
+      const float base = shift - m;
+      float sum = 0.f;
+      f16x8_t p[4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x = __builtin_amdgcn_exp2f(fmaf(s[u][e], f, base));
+          if (mask) {
+            const int t = t0 + 32 * u + 16 * (e / 8) + 8 * half + e % 8;
+            x = t >= see_lo && t < see_hi ? x : 0.f;
+          }
+          sum += x;
+          p[2 * u + e / 8][e % 8] = (_Float16)x;
+        }
+      // (a row that sees nothing of the tile keeps its sum, whatever the scale)
+      if (sum != 0.f) l = fmaf(sum, __builtin_amdgcn_exp2f(-shift), l);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8_t*>(vl + (k * kDt + d) * 1024), p[k], o[d], 0, 0, 0);
+    }
+    there = there_after;
+    k_scale = k_after;
+    v_scale = v_after;
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (!on) return;
+  const float back = v_ref * 0x1p-7f;                    // of the sums
+  // a block's channels 8 q + 4 half + j
+  if (n_chunk > 1) {
+    const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk + chunk;
+    const long n_slot = (long)gridDim.y * a.q_tiles * a.c.n_kv * a.n_chunk;
+    float* to = a.part + (slot * ROWS + r - it.r0) * D;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4_t*>(to + 32 * d + 8 * q + 4 * half) =
+            f32x4_t{o[d][4 * q] * back, o[d][4 * q + 1] * back, o[d][4 * q + 2] * back, o[d][4 * q + 3] * back};
+    if (half == 0) {
+      float* ml = a.part + n_slot * ROWS * D + (slot * ROWS + r - it.r0) * 2;
+      ml[0] = l == 0.f ? -__builtin_huge_valf() : m;
+      ml[1] = l;
+    }
+  } else {
+    T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D;
+    const float f = l == 0.f ? 0.f : back / l;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        attn_store4(to + 32 * d + 8 * q + 4 * half, f32x4_t{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]} * f, a.vec_o);
+    if (a.lse && half == 0)
+      a.lse[(long)(it.first + i) * a.n_q + head] = l == 0.f ? -__builtin_huge_valf() : (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
 
+// Joins the chunks of a row.  One work-group per row: D / 4 threads hold four values of it each, and kParts such sets take every
+// kParts-th chunk; their sums meet in LDS in order.
+template <typename T, int D, int ROWS>
+__global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
+  constexpr int kQuads = D / 4, kParts = kAttnThreads / kQuads;
+  __shared__ f32x4_t sum_s[kParts][kQuads];
+  __shared__ float weight_s[kAttnMostChunks], top_s[kAttnWaves], l_s[kAttnWaves];
+  const int r = blockIdx.x % ROWS, item = blockIdx.x / ROWS;
+  const int h = item % a.c.n_kv, q_tile = item / a.c.n_kv, seq = blockIdx.y;
+  const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
+  if (!it.there || it.r0 + r >= it.rows) return;         // uniform
+  const int n_chunk = attn_chunks(it, a.chunk_tiles);
+  if (n_chunk <= 1) return;                              // written by the first launch
+  const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk;
+  const long n_slot = (long)gridDim.y * a.q_tiles * a.c.n_kv * a.n_chunk;
+  const float* ml = a.part + n_slot * ROWS * D + (slot * ROWS + r) * 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float m[kAttnMostChunks / kAttnThreads], l[kAttnMostChunks / kAttnThreads], top = -__builtin_huge_valf();
+#pragma unroll
+  for (int k = 0; k < kAttnMostChunks / kAttnThreads; ++k) {
+    const int c = k * kAttnThreads + tid;
+    m[k] = c < n_chunk ? ml[(long)c * ROWS * 2] : -__builtin_huge_valf();
+    l[k] = c < n_chunk ? ml[(long)c * ROWS * 2 + 1] : 0.f;
+    top = fmaxf(top, m[k]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane == 0) top_s[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kAttnWaves; ++w) top = fmaxf(top, top_s[w]);
+  float total = 0.f;
+#pragma unroll
+  for (int k = 0; k < kAttnMostChunks / kAttnThreads; ++k) {
+    const int c = k * kAttnThreads + tid;
+    // a chunk that saw nothing has zero sums (or a NaN, which stays)
+    const float f = m[k] == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m[k] - top);
+    if (c < n_chunk) weight_s[c] = f;
+    total += l[k] * f;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+  if (lane == 0) l_s[wave] = total;
+  __syncthreads();
+  total = 0.f;
+#pragma unroll
+  for (int w = 0; w < kAttnWaves; ++w) total += l_s[w];
+  const int quad = tid % kQuads, first = tid / kQuads;
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  const float* from = a.part + (slot * ROWS + r) * D + 4 * quad;
+#pragma unroll 4
+  for (int c = first; c < n_chunk; c += kParts) {
+    const f32x4_t part = *reinterpret_cast<const f32x4_t*>(from + (long)c * ROWS * D);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(part[e], weight_s[c], v[e]);
+  }
+  sum_s[first][quad] = v;
+  __syncthreads();
+  if (first > 0) return;
+#pragma unroll
+  for (int k = 1; k < kParts; ++k) v += sum_s[k][quad];
+  const int i = (it.r0 + r) / a.group, head = h * a.group + (it.r0 + r) % a.group;
+  T* to = static_cast<T*>(a.out) + (long)(it.first + i) * a.ldo + (long)head * D + 4 * quad;
+  const float f = total == 0.f ? 0.f : 1.f / total;
+  attn_store4(to, v * f, a.vec_o);
+  if (a.lse && quad == 0)
+    a.lse[(long)(it.first + i) * a.n_q + head] = total == 0.f ? -__builtin_huge_valf() : (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
 // How a call is laid out: rows to a work item, work items along the queries, chunks along the cache.
+#ifndef ATTN_GROUPS
+#define ATTN_GROUPS 1536
+#endif
+constexpr int kAttnGroups = ATTN_GROUPS;
+
 struct AttnPlan {
   int rows, q_tiles, n_chunk, chunk_tiles;
   size_t ws_bytes;
@@ -355,17 +720,19 @@ static int attn_window(int window, int max_kv) { return window < max_kv ? window
 static AttnPlan attn_plan(int n_seq, int max_q, int max_kv, int n_q, int n_kv, int dim, int window) {
   AttnPlan p;
   const long rows = (long)max_q * (n_q / n_kv);
-  p.rows = rows <= 16 ? 16 : 32;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
   p.q_tiles = (int)((rows + p.rows - 1) / p.rows);
   // tiles that a work item can see
   window = attn_window(window, max_kv);
   long span = max_kv;
   if (window > 0 && window + (long)max_q < span) span = window + (long)max_q;
   const int tiles = (int)((span + kKvTile - 1) / kKvTile) + (window > 0 ? 1 : 0);
-  // 1024 work-groups, four to a CU, with at least eight tiles each
+  // kAttnGroups work-groups; a chunk has at least a tile for each wavefront, or four where there are enough work items to begin with
   const long items = (long)n_seq * n_kv * p.q_tiles;
-  long n = (1024 + items - 1) / items;
-  n = n < tiles / 8 ? n : tiles / 8;
+  const int least = items >= 256 ? 4 * kAttnWaves : kAttnWaves;
+  long n = (kAttnGroups + items - 1) / items;
+  n = n < tiles / least ? n : tiles / least;
+  n = n < kAttnMostChunks ? n : kAttnMostChunks;
   n = n > 1 ? n : 1;
   p.chunk_tiles = bpdq_ceil_div(bpdq_ceil_div(tiles > 0 ? tiles : 1, (int)n), kAttnWaves) * kAttnWaves;
   p.n_chunk = bpdq_ceil_div(tiles > 0 ? tiles : 1, p.chunk_tiles);
@@ -376,13 +743,20 @@ static AttnPlan attn_plan(int n_seq, int max_q, int max_kv, int n_q, int n_kv, i
 template <typename T, int D>
 static int attn_launch(const AttnArgs& a, const AttnPlan& p, int n_seq, hipStream_t stream) {
   const dim3 grid((unsigned)(p.q_tiles * a.c.n_kv * p.n_chunk), n_seq);
-  if (p.rows == 16) hipLaunchKernelGGL((attn_rows_kernel<T, D, 1>), grid, dim3(kAttnThreads), 0, stream, a);
-  else hipLaunchKernelGGL((attn_rows_kernel<T, D, 2>), grid, dim3(kAttnThreads), 0, stream, a);
+  if (p.rows == 16) {
+    hipLaunchKernelGGL((attn_rows_kernel<T, D, 1>), grid, dim3(kAttnThreads), 0, stream, a);
+  } else if (p.rows == 32) {
+    hipLaunchKernelGGL((attn_rows_kernel<T, D, 2>), grid, dim3(kAttnThreads), 0, stream, a);
+  } else {
+    BPDQ_HIP_TRY((bpdq_lds_limit<&attn_prompt_kernel<T, D>>(AttnPrompt<T, D>::kLds)));
+    hipLaunchKernelGGL((attn_prompt_kernel<T, D>), grid, dim3(kAttnThreads), (AttnPrompt<T, D>::kLds), stream, a);
+  }
   BPDQ_LAUNCH_CHECK();
   if (p.n_chunk > 1) {
-    const dim3 join((unsigned)(p.q_tiles * a.c.n_kv), n_seq, bpdq_ceil_div(p.rows * (D / 4), kAttnThreads));
+    const dim3 join((unsigned)(p.q_tiles * a.c.n_kv * p.rows), n_seq);
     if (p.rows == 16) hipLaunchKernelGGL((attn_join_kernel<T, D, 16>), join, dim3(kAttnThreads), 0, stream, a);
-    else hipLaunchKernelGGL((attn_join_kernel<T, D, 32>), join, dim3(kAttnThreads), 0, stream, a);
+    else if (p.rows == 32) hipLaunchKernelGGL((attn_join_kernel<T, D, 32>), join, dim3(kAttnThreads), 0, stream, a);
+    else hipLaunchKernelGGL((attn_join_kernel<T, D, 128>), join, dim3(kAttnThreads), 0, stream, a);
     BPDQ_LAUNCH_CHECK();
   }
   return 0;
@@ -433,7 +807,9 @@ extern "C" int bpdq_kv_attention(const bpdq_kv_cache* cache, const int* page_tab
   if (!out || (reinterpret_cast<uintptr_t>(out) & 1)) return -17;
   if (ldo < row) return -18;
   const AttnPlan p = attn_plan(n_seq, max_q, max_kv, n_q, cache->n_kv, cache->head_dim, window);
-  if ((long)p.q_tiles * cache->n_kv * p.n_chunk * kAttnThreads > 0xffffffffL) return -8;      // threads along the grid's x
+  // threads along the grids' x
+  if ((long)p.q_tiles * cache->n_kv * p.n_chunk * kAttnThreads > 0xffffffffL) return -8;
+  if (p.n_chunk > 1 && (long)p.q_tiles * cache->n_kv * p.rows * kAttnThreads > 0xffffffffL) return -8;
   if (p.ws_bytes && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))) return -20;
   if (ws_bytes < p.ws_bytes) return -21;
   AttnArgs a;
@@ -454,6 +830,8 @@ extern "C" int bpdq_kv_attention(const bpdq_kv_cache* cache, const int* page_tab
   a.n_q = n_q;
   a.group = group;
   a.causal = causal != 0;
+  a.vec_q = reinterpret_cast<uintptr_t>(Q) % 16 == 0 && ldq % 8 == 0;
+  a.vec_o = reinterpret_cast<uintptr_t>(out) % 8 == 0 && ldo % 4 == 0;
   a.window = attn_window(window, max_kv);
   a.q_tiles = p.q_tiles;
   a.n_chunk = p.n_chunk;
