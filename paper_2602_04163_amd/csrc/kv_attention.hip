@@ -39,6 +39,7 @@ struct AttnArgs {
   long ldq, ldo;
   int max_pages, n_tok, max_q, max_kv, n_q, group;
   int causal, window;
+  int page_shift;                                        // tiles of a page, as a power of two
   int vec_q, vec_o;                                      // whether Q goes by 16 bytes, and out by four values
   int q_tiles, n_chunk, chunk_tiles;
   float scale;
@@ -85,17 +86,11 @@ __device__ __forceinline__ int attn_chunks(const AttnItem& it, int chunk_tiles) 
 
 // eight codes (bytes of two words) as fp16
 __device__ __forceinline__ f16x8_t attn_codes(uint32_t a, uint32_t b) {
-  const uint32_t w[4] = {__builtin_amdgcn_perm(0x64646464u, a, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u),
-                         __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)};
   const f16x2_t zero = {(_Float16)1152.f, (_Float16)1152.f};
-  f16x8_t out;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const f16x2_t v = __builtin_bit_cast(f16x2_t, w[q]) - zero;
-    out[2 * q] = v[0];
-    out[2 * q + 1] = v[1];
-  }
-  return out;
+  auto two = [&](uint32_t bytes, uint32_t which) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, bytes, which)) - zero);
+  };
+  return __builtin_bit_cast(f16x8_t, u32x4_t{two(a, 0x04010400u), two(a, 0x04030402u), two(b, 0x04010400u), two(b, 0x04030402u)});
 }
 
 template <typename T>
@@ -121,7 +116,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
   const int chunk = blockIdx.x % a.n_chunk;
   const int item = blockIdx.x / a.n_chunk;               // (head, query tile)
   const int h = item % a.c.n_kv, q_tile = item / a.c.n_kv, seq = blockIdx.y;
-  const int per_page = a.c.page / kKvTile;
+  const int page_shift = a.page_shift, page_mask = (1 << page_shift) - 1;           // tiles of a page
   const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
   if (!it.there) return;                                 // uniform
   const int n_chunk = attn_chunks(it, a.chunk_tiles);
@@ -192,7 +187,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
   const int* row_of_table = a.table + (long)seq * a.max_pages;
   auto page_from = [&](int& tile) {                      // of the next tile from `tile` on that is there, or -1
     for (; tile < t_end; tile += kAttnWaves) {
-      const int id = row_of_table[tile / per_page];
+      const int id = row_of_table[tile >> page_shift];
       if (id >= 0 && id < a.c.n_pages) return id;
     }
     return -1;
@@ -202,7 +197,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
   float k_scale = 0.f, v_scale = 0.f;
   auto load_k = [&](int id, int tile) {
     at = (long)id * a.c.n_kv + h;
-    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.k + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.k + at * a.c.page * D + (long)(tile & page_mask) * kKvTile * D) + lane;
 #pragma unroll
     for (int n = 0; n < 4 * C; ++n) kw[n] = from[n * 64];
   };
@@ -211,7 +206,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
   if (id >= 0) load_k(id, tile);
   while (id >= 0) {
     {
-      const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.v + at * a.c.page * D + (long)(tile % per_page) * kKvTile * D) + lane;
+      const u32x4_t* from = reinterpret_cast<const u32x4_t*>(a.c.v + at * a.c.page * D + (long)(tile & page_mask) * kKvTile * D) + lane;
 #pragma unroll
       for (int d = 0; d < DT; ++d) vw[d] = from[d * 64];
     }
@@ -368,9 +363,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
 template <typename T, int D>
 struct AttnPrompt {
   static constexpr int kRows = 128, kKs = D / 16, kDt = D / 32;
-  static constexpr int kBuf = 2 * kKvTile * D * 2;       // bytes of a tile's K and V as fp16
+  static constexpr int kBuf = kKvTile * D * 2;           // bytes of a tile's K, and of its V, as fp16
   static constexpr int kChunks = kKvTile * D / 16 / kAttnThreads;   // 16-byte chunks of K, and of V, of a thread
-  static constexpr size_t kLds = 2 * kBuf;
+  static constexpr size_t kLds = 4 * kBuf;               // two of each
 };
 
 template <typename T, int D>
@@ -385,7 +380,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
   const int item = blockIdx.x / a.n_chunk;
   // the last queries see most: they go first
   const int h = item % a.c.n_kv, q_tile = a.q_tiles - 1 - item / a.c.n_kv, seq = blockIdx.y;
-  const int per_page = a.c.page / kKvTile;
+  const int page_shift = a.page_shift, page_mask = (1 << page_shift) - 1;           // tiles of a page
   const AttnItem it = attn_item<ROWS>(a, seq, q_tile);
   if (!it.there) return;                                 // uniform
   const int n_chunk = attn_chunks(it, a.chunk_tiles);
@@ -451,42 +446,58 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_hi = __builtin_amdgcn_readfirstlane(all_hi);
 
-  // The thread's chunks of a tile, and where they lie in LDS.  K: of 32 rows and 16 channels, [32 tokens][16 channels][half][row]; V: of 16
-  // tokens and 32 channels, [16 tokens][32 channels][half][channel].
-  u32x4_t kw[kChunks], vw[kChunks];
-  float k_scale = 0.f, v_scale = 0.f, k_scale_next = 0.f, v_scale_next = 0.f;
-  bool there = false, there_next = false;
+  // Pages and scales of the tiles from `known` on, one to a lane; -1 where there is nothing to be seen (behind the last tile, or a page
+  // outside the cache).
   const int* row_of_table = a.table + (long)seq * a.max_pages;
-  auto load = [&](int tile) {                            // a page outside the cache: another one's data, not looked at
-    const int id = tile < t_end ? row_of_table[tile / per_page] : -1;
-    there_next = id >= 0 && id < a.c.n_pages;
-    if (!there_next) return;                             // uniform
-    const long at = (long)id * a.c.n_kv + h;
-    const long byte = at * a.c.page * D + (long)(tile % per_page) * kKvTile * D;
-    const u32x4_t* kp = reinterpret_cast<const u32x4_t*>(a.c.k + byte);
-    const u32x4_t* vp = reinterpret_cast<const u32x4_t*>(a.c.v + byte);
-#pragma unroll
-    for (int n = 0; n < kChunks; ++n) {
-      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;       // u: (32 tokens, 16 channels) or (16 tokens, 32 channels)
-      const int ut = u / kKs, ks = u % kKs;
-      const int jr = rr & 3, hh = rr >> 2 & 1, jq = rr >> 3 & 1, sl = rr >> 4;
-      kw[n] = kp[((2 * hh + jq) * kKs + ks) * 16 + 4 * (2 * ut + sl) + jr];
-      const int s = u % 4, dt = u / 4;
-      vw[n] = vp[((2 * dt + (rr >> 4)) * 4 + s) * 16 + (rr & 15)];
-    }
-    k_scale_next = a.c.k_scale[at];
-    const float scale = a.c.v_scale[at];
-    v_scale_next = scale < 0x1p-120f ? 0x1p-120f : scale;         // (of zeros; the exponent wants a logarithm)
+  int known = 0, page_of = -1;
+  float k_scale_of = 0.f, v_scale_of = 0.f;
+  auto learn = [&](int tile) {
+    known = tile;
+    page_of = tile + lane < t_end ? row_of_table[(tile + lane) >> page_shift] : -1;
+    if (page_of >= a.c.n_pages) page_of = -1;
+    const long at = (long)(page_of < 0 ? 0 : page_of) * a.c.n_kv + h;
+    k_scale_of = a.c.k_scale[at];
+    v_scale_of = a.c.v_scale[at];
   };
-  auto store = [&](int buf) {
-    char* to = lds + buf * P::kBuf;
+  auto lane_of = [](auto x, int tile) {
+    return __builtin_bit_cast(decltype(x), __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), tile));
+  };
+  // The thread's chunks of a tile, and where they lie in LDS.  K: of 32 rows and 16 channels, [32 tokens][16 channels][half][row]; V: of 16
+  // tokens and 32 channels, [16 tokens][32 channels][half][channel].  (Where there is no page, the first one's data, which no row sees.)
+  u32x4_t kw[kChunks], vw[kChunks];
+  auto from = [&](const uint8_t* base, int tile) {
+    const int id = lane_of(page_of, tile - known);
+    return reinterpret_cast<const u32x4_t*>(base + ((long)(id < 0 ? 0 : id) * a.c.n_kv + h) * a.c.page * D +
+                                            (long)(id < 0 ? 0 : tile & page_mask) * kKvTile * D);
+  };
+  auto load_k = [&](int tile) {
+    const u32x4_t* p = from(a.c.k, tile);
 #pragma unroll
     for (int n = 0; n < kChunks; ++n) {
-      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;
-      f16x8_t* k = reinterpret_cast<f16x8_t*>(to + u * 1024) + rr;
+      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;       // u: (32 tokens, 16 channels)
+      const int jr = rr & 3, hh = rr >> 2 & 1, jq = rr >> 3 & 1, sl = rr >> 4;
+      kw[n] = p[((2 * hh + jq) * kKs + u % kKs) * 16 + 4 * (2 * (u / kKs) + sl) + jr];
+    }
+  };
+  auto load_v = [&](int tile) {
+    const u32x4_t* p = from(a.c.v, tile);
+#pragma unroll
+    for (int n = 0; n < kChunks; ++n) {
+      const int u = (n * kAttnThreads + tid) >> 5, rr = tid & 31;       // u: (16 tokens u % 4, 32 channels)
+      vw[n] = p[((2 * (u / 4) + (rr >> 4)) * 4 + u % 4) * 16 + (rr & 15)];
+    }
+  };
+  auto store_k = [&](int buf, int n) {
+    {
+      f16x8_t* k = reinterpret_cast<f16x8_t*>(lds + buf * P::kBuf + ((n * kAttnThreads + tid) >> 5) * 1024) + (tid & 31);
       k[0] = attn_codes(kw[n][0], kw[n][1]);
       k[32] = attn_codes(kw[n][2], kw[n][3]);
-      f16x8_t* v = reinterpret_cast<f16x8_t*>(to + kKvTile * D * 2 + ((u % 4) * kDt + u / 4) * 1024) + rr;
+    }
+  };
+  auto store_v = [&](int buf, int n) {
+    {
+      const int u = (n * kAttnThreads + tid) >> 5;
+      f16x8_t* v = reinterpret_cast<f16x8_t*>(lds + (2 + buf) * P::kBuf + ((u % 4) * kDt + u / 4) * 1024) + (tid & 31);
       v[0] = attn_codes(vw[n][0], vw[n][1]);
       v[32] = attn_codes(vw[n][2], vw[n][3]);
     }
@@ -498,109 +509,144 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float m = -__builtin_huge_valf(), l = 0.f;             // reference and sum of the lane's row (half of its tokens)
-  float v_ref = 0.f;
-  if (t_begin < t_end) {
-    load(t_begin);
-    if (there_next) store(0);
-  }
-  there = there_next;
-  k_scale = k_scale_next;
-  v_scale = v_scale_next;
-  load(t_begin + 1);
-  __syncthreads();
-  for (int tile = t_begin; tile < t_end; ++tile) {
-    const int buf = (tile - t_begin) & 1, t0 = tile * kKvTile;
-    const char* kl = lds + buf * P::kBuf + 16 * lane;
-    const char* vl = kl + kKvTile * D * 2;
-    const bool work = there && t0 < any_hi && t0 + kKvTile > any_lo;      // uniform
-    f32x16_t s[2];
-    if (work) {
+  float v_ref = 0.f, v_inv = __builtin_huge_valf();
+  // Operands from LDS come kG at a time, a group ahead of their products; the barriers for the scheduler keep it so.
+  constexpr int kG = kDt > 2 ? kDt / 2 : kDt, kGroups = 4 * kDt / kG;
+  f16x8_t part[2][kG];
+  auto read_k = [&](int buf, int g) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+    for (int n = 0; n < kG; ++n) part[g & 1][n] = *reinterpret_cast<const f16x8_t*>(lds + buf * P::kBuf + 16 * lane + (g * kG + n) * 1024);
+  };
+  auto read_v = [&](int buf, int g) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+    for (int n = 0; n < kG; ++n)
+      part[g & 1][n] = *reinterpret_cast<const f16x8_t*>(lds + (2 + buf) * P::kBuf + 16 * lane + (g * kG + n) * 1024);
+  };
+  auto scores = [&](f32x16_t (&s)[2], int g) {           // of a group: products g kG .. of half u of the tokens, channels 16 k ..
 #pragma unroll
-        for (int k = 0; k < kKs; ++k)
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8_t*>(kl + (u * kKs + k) * 1024), qf[k], s[u], 0, 0, 0);
-      }
+    for (int n = 0; n < kG; ++n) {
+      const int u = (g * kG + n) / kKs, k = (g * kG + n) % kKs;
+      if (k == 0) s[u] = f32x16_t{};
+      s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(part[g & 1][n], qf[k], s[u], 0, 0, 0);
     }
-    if (there_next) store(buf ^ 1);
-    const bool there_after = there_next;
-    const float k_after = k_scale_next, v_after = v_scale_next;
-    load(tile + 2);
-    if (work) {
-      // scores of register e of half u: token t0 + 32 u + 16 (e / 8) + 8 half + e % 8
-      const bool mask = t0 < all_lo || t0 + kKvTile > all_hi;
-      const float f = k_scale * q_scale;
-      float top = -3.0e38f;
-      if (mask) {
+  };
+  // Of a tile: its scores while the tile before goes through its softmax; K is two tiles ahead of the products with V, V one.
+  f32x16_t s0[2], s1[2];
+  if (t_begin < t_end) {
+    learn(t_begin);
+    load_k(t_begin);
+    load_v(t_begin);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+    for (int n = 0; n < kChunks; ++n) {
+      store_k(0, n);
+      store_v(0, n);
+    }
+    load_k(t_begin + 1);
+    __syncthreads();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int t = t0 + 32 * u + 16 * (e / 8) + 8 * half + e % 8;
-            top = fmaxf(top, t >= see_lo && t < see_hi ? s[u][e] : -3.0e38f);
-          }
-      } else {
+    for (int g = 0; g < kGroups; ++g) {
+      read_k(0, g);
+      scores(s0, g);
+    }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-      }
-      top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
-      if (__any(top > m + 8.f)) {
-        const float m_new = fmaxf(m, top);
-        const float fade = m_new == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= fade;
-#pragma unroll
-        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= fade;
-      }
-      // (a scale of V that is not finite fails both comparisons, and then reaches the rows that see the tile through the exponent)
-      float ratio = v_scale / v_ref;
-      if (!(ratio <= 1.f && ratio >= 0x1p-10f)) {
-        // 2^64 bounds the sums: what was added under a scale that much larger stays what counts
-        const float ref = 2.f * v_scale;
-        const float by = v_ref / ref;
-        if (v_scale < __builtin_huge_valf() && by < 0x1p64f) {
-#pragma unroll
-          for (int d = 0; d < kDt; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[d][e] *= by;
-          v_ref = ref;
-        }
-        ratio = v_scale / v_ref;
-      }
-      const float shift = v_scale < __builtin_huge_valf() ? 7.f + __builtin_amdgcn_logf(ratio) : __builtin_nanf("");
-      const float base = shift - m;
-      float sum = 0.f;
-      f16x8_t p[4];
+    for (int n = 0; n < kChunks; ++n) store_k(1, n);
+    load_k(t_begin + 2);
+    load_v(t_begin + 1);
+    __syncthreads();
+  }
+  auto step = [&](int tile, f32x16_t (&s)[2], f32x16_t (&s_next)[2]) {
+    const int buf = (tile - t_begin) & 1, t0 = tile * kKvTile;
+    read_k(buf ^ 1, 0);
+    if (tile + 3 > known + 63) learn(tile);
+    const bool there = lane_of(page_of, tile - known) >= 0;
+    const float k_scale = lane_of(k_scale_of, tile - known);
+    float v_scale = lane_of(v_scale_of, tile - known);
+    const bool bad = !(k_scale < __builtin_huge_valf()) || !(v_scale < __builtin_huge_valf());
+    v_scale = fmaxf(v_scale, 0x1p-120f);                 // (of zeros: the exponent wants a logarithm)
+    float f = k_scale * q_scale;
+    // scores of register e of half u: token t0 + 32 u + 16 (e / 8) + 8 half + e % 8
+    if (t0 < all_lo || t0 + kKvTile > all_hi || bad || !there) {        // uniform
+      const int lo = see_lo - t0 - 8 * half, hi = there ? see_hi - t0 - 8 * half : lo;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float x = __builtin_amdgcn_exp2f(fmaf(s[u][e], f, base));
-          if (mask) {
-            const int t = t0 + 32 * u + 16 * (e / 8) + 8 * half + e % 8;
-            x = t >= see_lo && t < see_hi ? x : 0.f;
-          }
-          sum += x;
-          p[2 * u + e / 8][e % 8] = (_Float16)x;
+          const int t = 32 * u + 16 * (e / 8) + e % 8;
+          // a scale that is not finite reaches the rows that see the tile, and no others
+          s[u][e] = t >= lo && t < hi ? bad ? __builtin_nanf("") : s[u][e] : -__builtin_huge_valf();
         }
-      // (a row that sees nothing of the tile keeps its sum, whatever the scale)
-      if (sum != 0.f) l = fmaf(sum, __builtin_amdgcn_exp2f(-shift), l);
+      if (bad) f = 1.f;
+    }
+    f = fmaxf(f, 0x1p-126f);                             // what is hidden stays so under any scale
+    float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+    for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(s[0][e], s[1][e]), top);
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
+    if (__any(top > m + 8.f)) {
+      const float m_new = fmaxf(m, top);
+      const float fade = m_new == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= fade;
+#pragma unroll
+      for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= fade;
+    }
+    float ratio = bad ? 1.f : v_scale * v_inv;
+    if (!bad && !(ratio <= 1.f && ratio >= 0x1p-10f)) {  // uniform
+      // 2^64 bounds the sums: what was added under a scale that much larger stays what counts
+      const float ref = 2.f * v_scale, by = v_ref / ref;
+      if (by < 0x1p64f) {
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8_t*>(vl + (k * kDt + d) * 1024), p[k], o[d], 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= by;
+        v_ref = ref;
+        v_inv = 1.f / ref;
+      }
+      ratio = v_scale * v_inv;
     }
-    there = there_after;
-    k_scale = k_after;
-    v_scale = v_after;
+    const float shift = 7.f + __builtin_amdgcn_logf(ratio), undo = __builtin_amdgcn_exp2f(-shift);
+    const float base = m == -__builtin_huge_valf() ? shift : shift - m;
+    __builtin_amdgcn_sched_barrier(0);
+
+    // the next tile's scores beside this one's exponentials
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    f16x8_t p[4];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      if (g + 1 < kGroups) read_k(buf ^ 1, g + 1);
+      else read_v(buf, 0);
+      scores(s_next, g);
+#pragma unroll
+      for (int n = g * (32 / kGroups); n < (g + 1) * (32 / kGroups); ++n) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[n / 16][n % 16], f, base));
+        sum[n & 3] += x;
+        p[n / 8][n % 8] = (_Float16)x;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undo, l);
+    // K two tiles ahead and V one are made beside its products
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      if (g + 1 < kGroups) read_v(buf, g + 1);
+#pragma unroll
+      for (int n = 0; n < kG; ++n) {
+        const int k = (g * kG + n) / kDt, d = (g * kG + n) % kDt;
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(part[g & 1][n], p[k], o[d], 0, 0, 0);
+      }
+      if (g % 2 == 0 && g < 2 * kChunks) store_k(buf, g / 2);
+      if (g % 2 == 1 && g < 2 * kChunks) store_v(buf ^ 1, g / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    load_k(tile + 3);
+    load_v(tile + 2);
     __syncthreads();
+  };
+  for (int tile = t_begin; tile < t_end; tile += 2) {
+    step(tile, s0, s1);
+    if (tile + 1 < t_end) step(tile + 1, s1, s0);
   }
   l += __shfl_xor(l, 32, 64);
   if (!on) return;
@@ -707,7 +753,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(AttnArgs a) {
 #ifndef ATTN_GROUPS
 #define ATTN_GROUPS 1536
 #endif
-constexpr int kAttnGroups = ATTN_GROUPS;
+constexpr int kAttnGroups = ATTN_GROUPS, kAttnPromptGroups = 512;
 
 struct AttnPlan {
   int rows, q_tiles, n_chunk, chunk_tiles;
@@ -730,7 +776,7 @@ static AttnPlan attn_plan(int n_seq, int max_q, int max_kv, int n_q, int n_kv, i
   // kAttnGroups work-groups; a chunk has at least a tile for each wavefront, or four where there are enough work items to begin with
   const long items = (long)n_seq * n_kv * p.q_tiles;
   const int least = items >= 256 ? 4 * kAttnWaves : kAttnWaves;
-  long n = (kAttnGroups + items - 1) / items;
+  long n = ((p.rows == 128 ? kAttnPromptGroups : kAttnGroups) + items - 1) / items;
   n = n < tiles / least ? n : tiles / least;
   n = n < kAttnMostChunks ? n : kAttnMostChunks;
   n = n > 1 ? n : 1;
@@ -832,6 +878,7 @@ extern "C" int bpdq_kv_attention(const bpdq_kv_cache* cache, const int* page_tab
   a.causal = causal != 0;
   a.vec_q = reinterpret_cast<uintptr_t>(Q) % 16 == 0 && ldq % 8 == 0;
   a.vec_o = reinterpret_cast<uintptr_t>(out) % 8 == 0 && ldo % 4 == 0;
+  a.page_shift = cache->page == 64 ? 0 : cache->page == 128 ? 1 : 2;
   a.window = attn_window(window, max_kv);
   a.q_tiles = p.q_tiles;
   a.n_chunk = p.n_chunk;
