@@ -441,15 +441,26 @@ ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 def _rows(t, dtype, shape, name):
-    """A tensor of the given shape on the GPU whose rows (all axes but the first) are dense."""
-    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+    """The row stride of a tensor of the given shape on the GPU whose rows (all axes but the first) are dense."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise BpdqError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
+    strides = t.stride()
     step = 1
-    for axis in range(t.dim() - 1, 0, -1):
-        if t.shape[axis] > 1 and t.stride(axis) != step:
+    for axis in range(len(shape) - 1, 0, -1):
+        if strides[axis] != step and shape[axis] > 1:
             raise BpdqError(f"{name}: its rows must be dense")
-        step *= t.shape[axis]
-    return max(t.stride(0), step) if t.shape[0] > 1 else step
+        step *= shape[axis]
+    return max(strides[0], step) if shape[0] > 1 else step
+
+
+def _call(name, rc):
+    if rc:
+        _check(rc, name)
+
+
+def _scratch(nbytes, device):
+    """A workspace, or None where none is asked for."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def bpdq_linear_workspace_bytes(n_tok, d_in):
@@ -459,53 +470,57 @@ def bpdq_linear_workspace_bytes(n_tok, d_in):
 def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None, Y=None, ws=None):
     """Y = act(X What^T + bias) + residual from the stored format, for any number of tokens; X, bias, residual and Y float16 or
     bfloat16.  Y may be the residual."""
-    lib = load()
+    lib = _lib or load()
     _dev(planes, torch.int32, "planes")
     _dev(coefs_h, torch.float16, "coefs_h")
     bits, d_out, nw = planes.shape
-    d_in = nw * 32
-    if coefs_h.shape != (bits + 1, d_out, d_in // group):
+    d_in, dtype = nw * 32, X.dtype
+    if group <= 0 or coefs_h.shape != (bits + 1, d_out, d_in // group):
         raise BpdqError("coefs_h: expected (bits + 1) x d_out x (d_in / group)")
-    if X.dim() != 2 or X.dtype not in (torch.float16, torch.bfloat16):
+    if X.dim() != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
         raise BpdqError("X: expected a float16 or bfloat16 matrix")
-    if act not in ACTS:
+    code = ACTS.get(act)
+    if code is None:
         raise BpdqError(f"act: expected one of {sorted(ACTS)}")
     n_tok = X.shape[0]
-    ldx = _rows(X, X.dtype, (n_tok, d_in), "X")
+    ldx = _rows(X, dtype, (n_tok, d_in), "X")
+    rows = (n_tok, d_out)
     if Y is None:
-        Y = torch.empty((n_tok, d_out), dtype=X.dtype, device=X.device)
-    ldy = _rows(Y, X.dtype, (n_tok, d_out), "Y")
-    if bias is not None:
-        _rows(bias, X.dtype, (d_out,), "bias")
-        if d_out > 1 and bias.stride(0) != 1:
-            raise BpdqError("bias: expected a dense vector")
-    if ws is None and n_tok > 32:
-        ws = _workspace(lib.bpdq_linear_workspace_bytes(n_tok, d_in), X.device)
-    ldr = 0 if residual is None else _rows(residual, X.dtype, (n_tok, d_out), "residual")
-    _check(lib.bpdq_linear(planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx,
-                           DTYPES[X.dtype], _ptr(bias), ACTS[act], _ptr(residual), ldr, Y.data_ptr(), ldy, _ptr(ws),
-                           0 if ws is None else ws.numel(), _stream()),
-           "bpdq_linear")
+        Y = torch.empty(rows, dtype=dtype, device=X.device)
+        ldy = d_out
+    else:
+        ldy = _rows(Y, dtype, rows, "Y")
+    if bias is not None and (bias.dtype is not dtype or bias.shape != (d_out,) or not bias.is_cuda or not bias.is_contiguous()):
+        raise BpdqError(f"bias: expected a contiguous {dtype} vector of d_out values on the GPU")
+    ldr = 0 if residual is None else _rows(residual, dtype, rows, "residual")
+    if ws is None:
+        ws = _scratch(lib.bpdq_linear_workspace_bytes(n_tok, d_in), X.device)
+    _call("bpdq_linear", lib.bpdq_linear(
+        planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx, DTYPES[dtype],
+        None if bias is None else bias.data_ptr(), code, None if residual is None else residual.data_ptr(), ldr, Y.data_ptr(), ldy,
+        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream()))
     return Y
 
 
 class KvCache:
     """Keys and values in 8 bits: k, v uint8 (n_pages, n_kv, page, head_dim) in the layout of include/bpdq.h, k_scale, v_scale
     float32 (n_pages, n_kv).  KvCache.empty(...) makes one."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "_c")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "n_kv", "page", "head_dim", "device", "_c", "_ref")
 
     def __init__(self, k, v, k_scale, v_scale):
         if k.dim() != 4:
             raise BpdqError("k: expected n_pages x n_kv x page x head_dim")
-        for t, name in ((k, "k"), (v, "v")):
-            _dev(t, torch.uint8, name)
-        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _dev(t, torch.float32, name)
-        if v.shape != k.shape or k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+        _dev(k, torch.uint8, "k")
+        _dev(v, torch.uint8, "v")
+        _dev(k_scale, torch.float32, "k_scale")
+        _dev(v_scale, torch.float32, "v_scale")
+        n_pages, self.n_kv, self.page, self.head_dim = shape = k.shape
+        if v.shape != shape or k_scale.shape != (n_pages, self.n_kv) or v_scale.shape != (n_pages, self.n_kv):
             raise BpdqError("v as k, and scales of n_pages x n_kv, are expected")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        n_pages, n_kv, page, head_dim = k.shape
-        self._c = BpdqKvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages, n_kv, page, head_dim)
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self._c = BpdqKvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *shape[:1], self.n_kv,
+                              self.page, self.head_dim)
+        self._ref = ctypes.byref(self._c)
 
     @classmethod
     def empty(cls, n_pages, n_kv, head_dim, page=64, device="cuda"):
@@ -514,47 +529,47 @@ class KvCache:
                    torch.empty(shape[:2], device=device), torch.empty(shape[:2], device=device))
 
 
-def _sequences(cache, page_table, at, start):
+def _sequences(page_table, at, start):
     """Checks of what describes the sequences of a call; their number and the table's width."""
     _dev(page_table, torch.int32, "page_table")
     _dev(at, torch.int32, "pos / kv_len")
     _dev(start, torch.int32, "tok_start / q_start")
     n_seq = at.numel()
-    if page_table.dim() != 2 or page_table.shape[0] != n_seq or start.numel() != n_seq + 1:
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] != n_seq or start.numel() != n_seq + 1:
         raise BpdqError("page_table: expected n_seq x max_pages, and n_seq + 1 starts")
-    return n_seq, page_table.shape[1]
+    return n_seq, shape[1]
 
 
 def bpdq_kv_write(cache, page_table, pos, tok_start, K, V, max_tok=None):
     """Quantizes rows tok_start[b] .. tok_start[b+1]-1 of K and V (n_tok, n_kv, head_dim) into the cache as tokens pos[b] .. of
     sequence b.  max_tok: at least the largest count of a sequence (all rows, if it is not given)."""
-    n_seq, max_pages = _sequences(cache, page_table, pos, tok_start)
-    c = cache._c
+    n_seq, max_pages = _sequences(page_table, pos, tok_start)
+    dtype = K.dtype
     n_tok = K.shape[0]
-    shape = (n_tok, c.n_kv, c.head_dim)
-    if K.dtype not in DTYPES:
+    shape = (n_tok, cache.n_kv, cache.head_dim)
+    if dtype not in DTYPES:
         raise BpdqError("K: expected float32, float16 or bfloat16")
-    ldk, ldv = _rows(K, K.dtype, shape, "K"), _rows(V, K.dtype, shape, "V")
-    _check(load().bpdq_kv_write(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(),
-                                n_tok, n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv,
-                                DTYPES[K.dtype], _stream()), "bpdq_kv_write")
+    ldk, ldv = _rows(K, dtype, shape, "K"), _rows(V, dtype, shape, "V")
+    _call("bpdq_kv_write", (_lib or load()).bpdq_kv_write(
+        cache._ref, page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(), n_tok,
+        n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv, DTYPES[dtype], _stream()))
 
 
 def bpdq_kv_read(cache, page_table, pos, tok_start, n_tok, max_tok=None, dtype=torch.float32, K=None, V=None):
     """Tokens pos[b] .. of sequence b from the cache into rows tok_start[b] .. tok_start[b+1]-1 of K and V; returns both."""
-    n_seq, max_pages = _sequences(cache, page_table, pos, tok_start)
-    c = cache._c
-    shape = (n_tok, c.n_kv, c.head_dim)
+    n_seq, max_pages = _sequences(page_table, pos, tok_start)
+    shape = (n_tok, cache.n_kv, cache.head_dim)
     if dtype not in DTYPES:
         raise BpdqError("dtype: expected float32, float16 or bfloat16")
     if K is None:
-        K = torch.empty(shape, dtype=dtype, device=cache.k.device)
+        K = torch.empty(shape, dtype=dtype, device=cache.device)
     if V is None:
-        V = torch.empty(shape, dtype=dtype, device=cache.k.device)
+        V = torch.empty(shape, dtype=dtype, device=cache.device)
     ldk, ldv = _rows(K, dtype, shape, "K"), _rows(V, dtype, shape, "V")
-    _check(load().bpdq_kv_read(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(),
-                               n_tok, n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv,
-                               DTYPES[dtype], _stream()), "bpdq_kv_read")
+    _call("bpdq_kv_read", (_lib or load()).bpdq_kv_read(
+        cache._ref, page_table.data_ptr(), max_pages, n_seq, pos.data_ptr(), tok_start.data_ptr(), n_tok,
+        n_tok if max_tok is None else max_tok, K.data_ptr(), ldk, V.data_ptr(), ldv, DTYPES[dtype], _stream()))
     return K, V
 
 
@@ -567,32 +582,34 @@ def bpdq_kv_attention(cache, page_table, kv_len, q_start, Q, max_q=None, max_kv=
     """Attention of rows q_start[b] .. q_start[b+1]-1 of Q (n_tok, n_q, head_dim), the last of them at position kv_len[b] - 1, over
     the kv_len[b] cached tokens of sequence b.  max_q, max_kv: at least the largest counts (all rows and all of the table's
     pages, if they are not given); scale: 1 / sqrt(head_dim) by default; lse: float32 (n_tok, n_q), filled if given."""
-    lib = load()
-    n_seq, max_pages = _sequences(cache, page_table, kv_len, q_start)
-    c = cache._c
-    if Q.dim() != 3 or Q.dtype not in (torch.float16, torch.bfloat16):
+    lib = _lib or load()
+    n_seq, max_pages = _sequences(page_table, kv_len, q_start)
+    dtype, dim = Q.dtype, cache.head_dim
+    if Q.dim() != 3 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
         raise BpdqError("Q: expected a float16 or bfloat16 tensor of n_tok x n_q x head_dim")
     n_tok, n_q = Q.shape[:2]
-    shape = (n_tok, n_q, c.head_dim)
-    ldq = _rows(Q, Q.dtype, shape, "Q")
+    shape = (n_tok, n_q, dim)
+    ldq = _rows(Q, dtype, shape, "Q")
     if max_q is None:
         max_q = n_tok
     if max_kv is None:
-        max_kv = max_pages * c.page
+        max_kv = max_pages * cache.page
     if out is None:
-        out = torch.empty(shape, dtype=Q.dtype, device=Q.device)
-    ldo = _rows(out, Q.dtype, shape, "out")
+        out = torch.empty(shape, dtype=dtype, device=Q.device)
+        ldo = n_q * dim
+    else:
+        ldo = _rows(out, dtype, shape, "out")
     if lse is not None:
         _dev(lse, torch.float32, "lse")
         if lse.shape != (n_tok, n_q):
             raise BpdqError("lse: expected n_tok x n_q")
     if ws is None:
-        need = lib.bpdq_kv_attention_workspace_bytes(n_seq, max_q, max_kv, n_q, c.n_kv, c.head_dim, window)
-        ws = _workspace(need, Q.device) if need else None
-    _check(lib.bpdq_kv_attention(ctypes.byref(c), page_table.data_ptr(), max_pages, n_seq, kv_len.data_ptr(),
-                                 q_start.data_ptr(), n_tok, max_q, max_kv, Q.data_ptr(), ldq, n_q, DTYPES[Q.dtype],
-                                 c.head_dim ** -0.5 if scale is None else scale, int(bool(causal)), window, out.data_ptr(), ldo,
-                                 _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream()), "bpdq_kv_attention")
+        ws = _scratch(lib.bpdq_kv_attention_workspace_bytes(n_seq, max_q, max_kv, n_q, cache.n_kv, dim, window), Q.device)
+    _call("bpdq_kv_attention", lib.bpdq_kv_attention(
+        cache._ref, page_table.data_ptr(), max_pages, n_seq, kv_len.data_ptr(), q_start.data_ptr(), n_tok, max_q, max_kv,
+        Q.data_ptr(), ldq, n_q, DTYPES[dtype], dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
+        out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
+        0 if ws is None else ws.numel(), _stream()))
     return out
 
 

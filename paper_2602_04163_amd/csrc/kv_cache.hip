@@ -16,6 +16,7 @@
 namespace bpdq {
 
 constexpr int kKvThreads = 256;
+constexpr int kKvKeep = 2;
 constexpr float kKvFloor = 0x1p-96f;
 
 // 16 consecutive values as floats
@@ -30,20 +31,6 @@ __device__ __forceinline__ void kv_load16(const T* __restrict__ p, bool vec, flo
   } else {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = (float)p[e];
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ void kv_store16(T* __restrict__ p, bool vec, const float (&x)[16]) {
-  if (vec) {
-    alignas(16) T raw[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) raw[e] = (T)x[e];
-#pragma unroll
-    for (int q = 0; q < (int)sizeof(T); ++q) reinterpret_cast<u32x4_t*>(p)[q] = reinterpret_cast<const u32x4_t*>(raw)[q];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) p[e] = (T)x[e];
   }
 }
 
@@ -129,14 +116,28 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(bpdq_kv_cache c, c
   // the largest magnitude, as bits: a NaN is above an infinity, an infinity above every number
   const float old = s.lo > 0 ? *scale_at : 0.f;
   uint32_t most = 0;
-  for (int id = tid; id < items; id += kKvThreads) {
-    float x[16];
+  auto fetch = [&](int id, float (&x)[16]) {
     kv_load16(src + (s.row + s.lo + id / (D / 16)) * ld + 16 * (id % (D / 16)), vec, x);
+  };
+  auto look = [&](const float (&x)[16]) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const uint32_t b = __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu;
       most = most > b ? most : b;
     }
+  };
+  // a thread's first kKvKeep items (all of a page of 64 tokens of 128 channels) stay in registers, others are read again
+  float kept[kKvKeep][16];
+#pragma unroll
+  for (int n = 0; n < kKvKeep; ++n)
+    if (tid + n * kKvThreads < items) fetch(tid + n * kKvThreads, kept[n]);
+#pragma unroll
+  for (int n = 0; n < kKvKeep; ++n)
+    if (tid + n * kKvThreads < items) look(kept[n]);
+  for (int id = tid + kKvKeep * kKvThreads; id < items; id += kKvThreads) {
+    float x[16];
+    fetch(id, x);
+    look(x);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -171,16 +172,28 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(bpdq_kv_cache c, c
   if (tid == 0 && (s.lo == 0 || !(scale == old))) *scale_at = scale;
   const float inv = 1.f / scale;
 
-  if (!is_v) {
-    for (int id = tid; id < items; id += kKvThreads) {
-      const int t = s.lo + id / (D / 16), c16 = id % (D / 16);
-      float x[16];
-      kv_load16(src + (s.row + t) * ld + 16 * c16, vec, x);
-      u32x4_t w;
+  auto put = [&](int id, const float (&x)[16]) {
+    const int t = s.lo + id / (D / 16), c16 = id % (D / 16);
+    u32x4_t w;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = kv_pack4(x + 4 * q, inv);
+    for (int q = 0; q < 4; ++q) w[q] = kv_pack4(x + 4 * q, inv);
+    if (!is_v) {
       out[kv_k_chunk(t, c16, D)] = w;
+    } else {
+      uint32_t* to = reinterpret_cast<uint32_t*>(lds + t * kRow + 16 * c16);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) to[q] = w[q];
     }
+  };
+#pragma unroll
+  for (int n = 0; n < kKvKeep; ++n)
+    if (tid + n * kKvThreads < items) put(tid + n * kKvThreads, kept[n]);
+  for (int id = tid + kKvKeep * kKvThreads; id < items; id += kKvThreads) {
+    float x[16];
+    fetch(id, x);
+    put(id, x);
+  }
+  if (!is_v) {
     if (grew) {
       for (int id = tid; id < s.lo * (D / 16); id += kKvThreads) {
         u32x4_t* p = out + kv_k_chunk(id / (D / 16), id % (D / 16), D);
@@ -191,14 +204,6 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(bpdq_kv_cache c, c
       }
     }
     return;
-  }
-  for (int id = tid; id < items; id += kKvThreads) {
-    const int t = s.lo + id / (D / 16), c16 = id % (D / 16);
-    float x[16];
-    kv_load16(src + (s.row + t) * ld + 16 * c16, vec, x);
-    uint32_t* w = reinterpret_cast<uint32_t*>(lds + t * kRow + 16 * c16);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = kv_pack4(x + 4 * q, inv);
   }
   __syncthreads();
   // 16 slots of four channels at a time
@@ -259,9 +264,9 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(bpdq_kv_cache c, co
   const long at = (long)(s.phys < 0 ? 0 : s.phys) * c.n_kv + h;
   const u32x4_t* in = reinterpret_cast<const u32x4_t*>((is_v ? c.v : c.k) + at * c.page * D);
   const float scale = s.phys < 0 ? 0.f : (is_v ? c.v_scale : c.k_scale)[at];
-  const int items = (s.hi - s.lo) * (D / 16);
 
-  if (is_v && s.phys >= 0) {
+  // codes to LDS by slot, as they lie in the cache
+  if (s.phys >= 0 && is_v) {
     const int s16_lo = s.lo / 16, s16_n = (s.hi + 15) / 16 - s16_lo;
     for (int id = tid; id < s16_n * (D / 4); id += kKvThreads) {
       const int s16 = s16_lo + id / (D / 4), d = 4 * (id % (D / 4));
@@ -275,23 +280,37 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(bpdq_kv_cache c, co
         for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(lds + (16 * s16 + 4 * q + i) * kRow + d) = row[i];
       }
     }
-    __syncthreads();
-  }
-  for (int id = tid; id < items; id += kKvThreads) {
-    const int t = s.lo + id / (D / 16), c16 = id % (D / 16);
-    u32x4_t w = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-    if (s.phys >= 0) {
-      if (is_v) {
-        const uint32_t* r = reinterpret_cast<const uint32_t*>(lds + t * kRow + 16 * c16);
-        w = u32x4_t{r[0], r[1], r[2], r[3]};
-      } else {
-        w = in[kv_k_chunk(t, c16, D)];
-      }
-    }
-    float x[16];
+  } else if (s.phys >= 0) {
+    const int tile_lo = s.lo / kKvTile, tile_n = (s.hi + kKvTile - 1) / kKvTile - tile_lo;
+    for (int id = tid; id < tile_n * 4 * D; id += kKvThreads) {
+      const int at = id % (4 * D), c16 = at / 16 % (D / 16);
+      const int t = (tile_lo + id / (4 * D)) * kKvTile + 16 * (at / 4 % 4) + 4 * (at / D) + at % 4;
+      if (t < s.lo || t >= s.hi) continue;
+      const u32x4_t w = in[(tile_lo * 4 * D) + id];
+      uint32_t* to = reinterpret_cast<uint32_t*>(lds + t * kRow + 16 * c16);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = (float)((int)((w[e / 4] >> (8 * (e % 4))) & 255u) - 128) * scale;
-    kv_store16(dst + (s.row + t) * ld + 16 * c16, vec, x);
+      for (int q = 0; q < 4; ++q) to[q] = w[q];
+    }
+  }
+  __syncthreads();
+  // and out, 16 bytes a lane, consecutive lanes consecutive channels
+  constexpr int kVec = 16 / sizeof(T);
+  for (int id = tid; id < (s.hi - s.lo) * (D / kVec); id += kKvThreads) {
+    const int t = s.lo + id / (D / kVec), d = kVec * (id % (D / kVec));
+    alignas(16) T out[kVec];
+#pragma unroll
+    for (int q = 0; q < kVec / 4; ++q) {
+      const uint32_t w = s.phys >= 0 ? *reinterpret_cast<const uint32_t*>(lds + t * kRow + d + 4 * q) : 0x80808080u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * q + e] = (T)((float)((int)((w >> (8 * e)) & 255u) - 128) * scale);
+    }
+    T* to = dst + (s.row + t) * ld + d;
+    if (vec) {
+      *reinterpret_cast<u32x4_t*>(to) = *reinterpret_cast<const u32x4_t*>(out);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) to[e] = out[e];
+    }
   }
 }
 
