@@ -237,9 +237,9 @@ int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_
  *   X : n_tok x d_in, row stride ldx;  bias : d_out or NULL;  residual : n_tok x d_out, row stride ldr, or NULL;
  *   Y : n_tok x d_out, row stride ldy.  All of one type, BPDQ_F16 or BPDQ_BF16 (uint16 bit patterns); strides in elements.
  *   act : BPDQ_ACT_*; GELU is v Phi(v), GELU_TANH its approximation by tanh, SILU v / (1 + exp(-v)).
- * What is evaluated in fp32 and rounded once to the type of X; the products are exact, sums, bias, activation and residual
- * fp32; Y is rounded once.  (A level of a row outside the range of BPDQ_F16 becomes infinite there; it does not in
- * BPDQ_BF16.)  A NaN or infinity in a row of X reaches that row of Y alone.
+ * What is evaluated in fp32 and rounded once to fp16; X in bf16 is scaled by a power of two per token and taken as fp16, which changes no
+ * value above 2^-29 of the token's largest; the products are exact, sums, bias, activation and residual fp32; Y is rounded once.
+ * (A level of a row beyond 65504 becomes infinite.)  A NaN or infinity in a row of X reaches that row of Y alone.
  * Y may be the residual itself (same address and stride); other overlaps are not allowed.  The result of a token does not
  * depend on the others of the call beyond the choice of kernel by n_tok, which changes the order of sums.
  * From 33 tokens on X is brought into the order of the matrix instructions first, in ws: 256-byte aligned,

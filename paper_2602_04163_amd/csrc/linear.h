@@ -16,10 +16,13 @@ namespace bpdq {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kLinRowsMost = 32;                           // tokens of the kernel without an ordering of X
 constexpr int kLinTokPad = 256;                           // the ordering covers whole tiles of any shape
+
+static inline size_t linear_image_bytes(int n_tok, int d_in) {
+  return bpdq_align_up((size_t)n_tok, kLinTokPad) * bpdq_align_up((size_t)d_in, 256) * 2;
+}
 
 struct LinearArgs {
   const uint32_t* planes;
@@ -34,12 +37,43 @@ struct LinearArgs {
   int vec_x, vec_w, vec_r, vec_y;                        // whether X, the planes, the residual and Y go by 16 bytes
 };
 
-template <typename T>
 __device__ __forceinline__ f32x4_t mfma_16x16x32(u32x4_t a, u32x4_t b, f32x4_t c) {
-  if constexpr (__is_same(T, _Float16))
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+// X in bf16 as fp16.  Weights rounded to bf16 would cost as much accuracy again as the rounding of the result (measured: 1.4 to 1.6 times
+// the error); fp16 has the bits of both, and a power of two per token brings its values into range, exactly but for those below 2^-29 of the token's
+// largest.  The largest magnitude's exponent goes to that of [2^15, 2^16), on the bit patterns: pattern - base, in units of an
+// exponent, saturating at zero, and three bits up.  (A row with an infinity or NaN keeps these.)
+__device__ __forceinline__ uint32_t linear_base(uint32_t most) {        // of the token's largest pattern without sign
+  const int e = most >> 7;
+  return e == 255 ? 224u << 7 : e > 30 ? (uint32_t)(e - 30) << 7 : 0u;
+}
+__device__ __forceinline__ float linear_unscale(uint32_t base) { return ldexpf(1.f, (int)(base >> 7) - 112); }
+__device__ __forceinline__ uint32_t linear_half2(uint32_t x, uint32_t base2) {       // base2: base in both halves
+  typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+  const u16x2_t m = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2_t, x & 0x7fff7fffu), __builtin_bit_cast(u16x2_t, base2));
+  return __builtin_bit_cast(uint32_t, m) << 3 | (x & 0x80008000u);
+}
+// the larger of the eight patterns without sign and of `most`
+__device__ __forceinline__ uint32_t linear_most(u32x4_t v, uint32_t most) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t a = v[q] & 0x7fffu, b = v[q] >> 16 & 0x7fffu;
+    most = most > a ? most : a;
+    most = most > b ? most : b;
+  }
+  return most;
+}
+// eight consecutive values of X
+template <typename T>
+__device__ __forceinline__ u32x4_t linear_load8(const T* __restrict__ x, bool vec) {
+  if (vec) return *reinterpret_cast<const u32x4_t*>(x);
+  const unsigned short* s = reinterpret_cast<const unsigned short*>(x);
+  u32x4_t v;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = (uint32_t)s[2 * q] | (uint32_t)s[2 * q + 1] << 16;
+  return v;
 }
 
 template <int ACT>
@@ -72,36 +106,6 @@ __device__ __forceinline__ float linear_act(float v, int act) {
   }
 }
 
-// 32 columns of a row of X, zeros from column d_in on (`columns` of them are there)
-template <typename T>
-__device__ __forceinline__ void linear_load_x(const T* __restrict__ x, int columns, bool vec, uint32_t (&out)[16]) {
-  if (columns <= 0) {
-#pragma unroll
-    for (int q = 0; q < 16; ++q) out[q] = 0;
-  } else if (vec) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const u32x4_t v = reinterpret_cast<const u32x4_t*>(x)[q];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) out[4 * q + e] = v[e];
-    }
-  } else {
-    const unsigned short* s = reinterpret_cast<const unsigned short*>(x);
-#pragma unroll
-    for (int q = 0; q < 16; ++q) out[q] = (uint32_t)s[2 * q] | (uint32_t)s[2 * q + 1] << 16;
-  }
-}
-
-// four consecutive words of a plane's row, of which `words` are there, the others zero
-__device__ __forceinline__ u32x4_t linear_load_w(const uint32_t* __restrict__ p, int words, bool vec) {
-  if (vec && words >= 4) return *reinterpret_cast<const u32x4_t*>(p);
-  u32x4_t w = {0, 0, 0, 0};
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j < words) w[j] = p[j];
-  return w;
-}
-
 constexpr int kWords = 4;                                 // consecutive words of a lane in the tile kernel
 constexpr int kLinThreads = 512;
 constexpr int kLinWaves = kLinThreads / 64;
@@ -119,6 +123,8 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32;
   const int toks = a.n_tok - tok0 < kToks ? a.n_tok - tok0 : kToks;
   char* stage = reinterpret_cast<char*>(lds_raw) + wave * 16 * kRowPitch;
+  constexpr bool kScale = !__is_same(T, _Float16);
+  __shared__ uint32_t most_s[kLinWaves][kToks], base_s[kToks];
 
   f32x4_t acc[R][NT];
 #pragma unroll
@@ -149,6 +155,33 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
     load_c(r, word, c_next);
   };
   if (8 * wave < nw) load_w(0, 8 * wave + 2 * quarter);
+  if constexpr (kScale) {                                // (while the first words are on their way)
+    for (int t0 = 0; t0 < toks; t0 += 4) {
+      uint32_t most[4] = {0, 0, 0, 0};
+      for (int c = 8 * tid; c < a.d_in; c += 8 * kLinThreads)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (t0 + t < toks) most[t] = linear_most(linear_load8(static_cast<const T*>(a.x) + (tok0 + t0 + t) * a.ldx + c, a.vec_x), most[t]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (t0 + t >= toks) break;                       // uniform
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          const uint32_t b = __shfl_xor(most[t], o, 64);
+          most[t] = most[t] > b ? most[t] : b;
+        }
+        if (lane == 0) most_s[wave][t0 + t] = most[t];
+      }
+    }
+    __syncthreads();
+    if (tid < toks) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int w = 0; w < kLinWaves; ++w) most = most > most_s[w][tid] ? most : most_s[w][tid];
+      base_s[tid] = linear_base(most);
+    }
+    __syncthreads();
+  }
   for (int w0 = 8 * wave; w0 < nw; w0 += 8 * kLinWaves) {
     const int word = w0 + 2 * quarter;                   // the lane's words: word, word + 1
     // X of 256 columns to operands, 16 tokens at a time by way of LDS: loads of whole lines.  Rows behind the last token keep what LDS
@@ -162,19 +195,17 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
       for (int i = 0; i < 8; ++i) {
         if (16 * n + 2 * i >= toks) break;               // uniform
         const int t = 16 * n + 2 * i + (lane >> 5) < toks ? 16 * n + 2 * i + (lane >> 5) : toks - 1;
-        const T* x = static_cast<const T*>(a.x) + (tok0 + t) * a.ldx + (at < nw ? 8L * (4 * w0 + (lane & 31)) : 0L);
-        if (a.vec_x) {
-          v[i] = *reinterpret_cast<const u32x4_t*>(x);
-        } else {
-          const unsigned short* e = reinterpret_cast<const unsigned short*>(x);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) v[i][q] = (uint32_t)e[2 * q] | (uint32_t)e[2 * q + 1] << 16;
-        }
+        v[i] = linear_load8(static_cast<const T*>(a.x) + (tok0 + t) * a.ldx + (at < nw ? 8L * (4 * w0 + (lane & 31)) : 0L), a.vec_x);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (16 * n + 2 * i >= toks) break;
         if (at >= nw) v[i] = u32x4_t{0, 0, 0, 0};
+        if constexpr (kScale) {
+          const uint32_t base = base_s[16 * n + 2 * i + (lane >> 5) < toks ? 16 * n + 2 * i + (lane >> 5) : toks - 1] * 0x10001u;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[i][q] = linear_half2(v[i][q], base);
+        }
         *reinterpret_cast<u32x4_t*>(stage + (2 * i + (lane >> 5)) * kRowPitch + 16 * (lane & 31)) = v[i];
       }
       __builtin_amdgcn_wave_barrier();                   // (LDS serves a wavefront in order)
@@ -201,7 +232,7 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
       for (int i = 0; i <= K; ++i) c[i] = word < nw ? c_next[i] : (_Float16)0.f;      // words past the end add nothing
       if (r + 1 < R) load_w(r + 1, word);
       else if (w0 + 8 * kLinWaves < nw) load_w(0, word + 8 * kLinWaves);
-      PlaneLevels<T, K> levels;
+      PlaneLevels<K> levels;
       levels.set(c);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -217,9 +248,9 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
         const PlaneWord<K> pw(words);
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-          const u32x4_t v = pw.template values<T>(levels, f);
+          const u32x4_t v = pw.values(levels, f);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) acc[r][n] = mfma_16x16x32<T>(v, xs[n][j][f], acc[r][n]);
+          for (int n = 0; n < NT; ++n) acc[r][n] = mfma_16x16x32(v, xs[n][j][f], acc[r][n]);
         }
       }
     }
@@ -239,6 +270,7 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
     float v = 0.f;
 #pragma unroll
     for (int s = 0; s < kLinWaves; ++s) v += part[s * kToks * kRows + id];
+    if constexpr (kScale) v *= linear_unscale(base_s[id / kRows]);
     if (a.bias) v += (float)static_cast<const T*>(a.bias)[r];
     v = linear_act(v, a.act);
     if (a.residual) v += (float)static_cast<const T*>(a.residual)[t * a.ldr + r];
@@ -246,12 +278,8 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
   }
 }
 
-template <typename T>
 __device__ __forceinline__ f32x16_t mfma_32x32x16(u32x4_t a, u32x4_t b, f32x16_t c) {
-  if constexpr (__is_same(T, _Float16))
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
 
 // One LDS-DMA load: 64 lanes x 16 bytes from `base + voff` (per lane) to the 1 KB of LDS that starts at byte address lds_addr
@@ -276,7 +304,7 @@ struct LinearTile {
   static constexpr int kAcc = 16 * RT * TT;              // accumulators of a lane
   static constexpr int kDma = kToks * 128 / 1024 / (WR * WT);       // requests of a wavefront per 64 columns
   static constexpr int kStage = kToks * 128;             // bytes of 64 columns of X
-  static constexpr int kLevel = 8 * PlaneLevels<_Float16, K>::kRegs;        // bytes of the levels of a row and group
+  static constexpr int kLevel = 8 * PlaneLevels<K>::kRegs;        // bytes of the levels of a row and group
   static constexpr int kTable = 2 * kRows * kLevel;      // of the rows' levels of a stage, one word for each half
   static constexpr int kRing = kStages * KS * kStage;
   static constexpr size_t kLds = (size_t)kRing + 2 * KS * kTable;
@@ -290,32 +318,60 @@ struct LinearTile {
 // of a step and half fall into all 64 banks of LDS.  Tokens from n_tok on and columns from d_in on are zero.
 // One wavefront per image.
 template <typename T>
-__global__ __launch_bounds__(256) void linear_order_kernel(LinearArgs a, int n_image, int images, u32x4_t* __restrict__ out) {
+__global__ __launch_bounds__(256) void linear_order_kernel(LinearArgs a, int n_image, int images, const uint32_t* __restrict__ base) {
   const int id = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= n_image) return;
   const int block = id / images, at = id % images;       // images: of a block of 32 tokens
   const int half = threadIdx.x & 1, t = (threadIdx.x & 63) >> 1;
   const int word = at / 4 * 8 + 4 * half + at % 4;
   const long tok = 32L * block + t;
+  const bool on = tok < a.n_tok && 32 * word < a.d_in;
+  const T* x = static_cast<const T*>(a.x) + (on ? tok * a.ldx + 32L * word : 0L);
   uint32_t raw[16];
-  linear_load_x(static_cast<const T*>(a.x) + (tok < a.n_tok ? tok : 0) * a.ldx + 32L * word,
-                tok < a.n_tok ? a.d_in - 32 * word : 0, a.vec_x, raw);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const u32x4_t v = linear_load8(x + 8 * q, a.vec_x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) raw[4 * q + e] = on ? v[e] : 0u;
+  }
+  if constexpr (!__is_same(T, _Float16)) {
+    const uint32_t base2 = on ? base[tok] * 0x10001u : 0u;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) raw[e] = linear_half2(raw[e], base2);
+  }
   u32x4_t step[4];
   plane_order(raw, step);
-  u32x4_t* to = out + (long)id * 256 + 8 * t;
+  u32x4_t* to = static_cast<u32x4_t*>(a.ws) + (long)id * 256 + 8 * t;
 #pragma unroll
   for (int f = 0; f < 4; ++f) to[(4 * half + f) ^ (t >> 1 & 7)] = step[f];
+}
+
+// Every token's base (linear_base), a wavefront each.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_base_kernel(LinearArgs a, uint32_t* __restrict__ base) {
+  const int tok = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (tok >= a.n_tok) return;
+  const T* x = static_cast<const T*>(a.x) + tok * a.ldx;
+  uint32_t most = 0;
+#pragma unroll 4
+  for (int c = 8 * lane; c < a.d_in; c += 512) most = linear_most(linear_load8(x + c, a.vec_x), most);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t b = __shfl_xor(most, o, 64);
+    most = most > b ? most : b;
+  }
+  if (lane == 0) base[tok] = linear_base(most);
 }
 
 // Eight rows from `first` of one token: bias, activation, residual, one rounding.
 template <typename T, int ACT>
 __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, int first, f32x4_t v0, f32x4_t v1,
-                                               const float (&bias)[8], bool vec_y, bool vec_r) {
+                                               float unscale, const float (&bias)[8], bool vec_y, bool vec_r) {
   typedef T T8 __attribute__((ext_vector_type(8)));
   float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
   const int n = a.d_out - first < 8 ? a.d_out - first : 8;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = linear_act<ACT>(v[i] + bias[i]);
+  for (int i = 0; i < 8; ++i) v[i] = linear_act<ACT>(v[i] * unscale + bias[i]);
   if (a.residual) {
     const T* r = static_cast<const T*>(a.residual) + tok * a.ldr + first;
     if (vec_r && n == 8) {
@@ -351,7 +407,7 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
 // The compiler does not see the LDS-DMA requests (inline assembly), so the vmcnt waits are written by hand: at most the requests of
 // the stages behind the next one may be outstanding.  Loads that the compiler issues meanwhile only make that wait longer.
 template <typename T, int K, typename S, int GS, bool VEC>
-__global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const char* __restrict__ images) {
+__global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const uint32_t* __restrict__ base) {
   constexpr int W = kWords, RT = S::RT, TT = S::TT;
   extern __shared__ uint4 lds_raw[];
   char* lds = reinterpret_cast<char*>(lds_raw);
@@ -366,7 +422,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
 
   // a stage: kToks / 32 images; the wavefront requests kDma runs of 1 KB.  Stages past the end repeat the last one.
   const int n_image = 4 * all_chunks;
-  const char* x_from = images + (long)(tok0 / 32) * n_image * 4096;
+  const char* x_from = static_cast<const char*>(a.ws) + (long)(tok0 / 32) * n_image * 4096;
   unsigned run_from[S::kDma];                            // of a run, in bytes from x_from (all of a tile within 32 bits)
 #pragma unroll
   for (int i = 0; i < S::kDma; ++i) {
@@ -427,7 +483,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   // Levels of the stages whose words begin a group: the part's threads make them for all rows, [half][row], from coefficients that
   // were requested when the levels before them were made.
   char* table = lds + S::kRing + part * 2 * S::kTable;
-  typedef uint32_t Level __attribute__((ext_vector_type(2 * PlaneLevels<T, K>::kRegs)));
+  typedef uint32_t Level __attribute__((ext_vector_type(2 * PlaneLevels<K>::kRegs)));
   constexpr int kUnits = 2 * S::kRows / S::kPart;        // (half, row) pairs of a thread
   _Float16 c_raw[kUnits][K + 1];
   auto level_word = [&](int stage, int h) { return 2 * W * (stage / W * S::KS + part) + W * h + stage % W; };
@@ -447,24 +503,24 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int u = 0; u < kUnits; ++u) {
       const int id = u * S::kPart + tid;
       const bool on = level_word(stage, id / S::kRows) < nw;        // words past the end add nothing
-      PlaneLevels<T, K> made;
+      PlaneLevels<K> made;
       made.set(c_raw[u]);
       Level out;
 #pragma unroll
-      for (int n = 0; n < PlaneLevels<T, K>::kRegs; ++n) {
+      for (int n = 0; n < PlaneLevels<K>::kRegs; ++n) {
         out[2 * n] = on ? made.lo[n] : 0u;
         out[2 * n + 1] = on ? made.hi[n] : 0u;
       }
       reinterpret_cast<Level*>(table + (stage & 1) * S::kTable)[id] = out;
     }
   };
-  PlaneLevels<T, K> levels[RT];
+  PlaneLevels<K> levels[RT];
   auto read_levels = [&](int stage) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const Level in = reinterpret_cast<const Level*>(table + (stage & 1) * S::kTable)[half * S::kRows + 32 * (RT * wr + r) + low];
 #pragma unroll
-      for (int n = 0; n < PlaneLevels<T, K>::kRegs; ++n) {
+      for (int n = 0; n < PlaneLevels<K>::kRegs; ++n) {
         levels[r].lo[n] = in[2 * n];
         levels[r].hi[n] = in[2 * n + 1];
       }
@@ -490,7 +546,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       uint32_t words[K];
 #pragma unroll
       for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][j];
-      v[f & 1][r] = PlaneWord<K>(words).template values<T>(levels[r], f);
+      v[f & 1][r] = PlaneWord<K>(words).values(levels[r], f);
     }
   };
 
@@ -540,7 +596,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
 #pragma unroll
-          for (int r = 0; r < RT; ++r) acc[r][t] = mfma_32x32x16<T>(v[f & 1][r], b[t], acc[r][t]);
+          for (int r = 0; r < RT; ++r) acc[r][t] = mfma_32x32x16(v[f & 1][r], b[t], acc[r][t]);
           read_b(f < 3 ? ring : ring1, (f + 1) & 3, t);
         }
 #pragma unroll
@@ -599,7 +655,8 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       const int k = it * 8 + (lane >> 3);
       const f32x4_t v0 = mine[k * 16 + (s2 ^ (k & 15))], v1 = mine[k * 16 + ((s2 + 1) ^ (k & 15))];
       const long tok = tok0 + 32 * (TT * wt + t) + k;
-      if (tok < a.n_tok && first < a.d_out) linear_finish8<T, act.value>(a, tok, first, v0, v1, bias, a.vec_y, a.vec_r);
+      if (tok < a.n_tok && first < a.d_out)
+        linear_finish8<T, act.value>(a, tok, first, v0, v1, __is_same(T, _Float16) ? 1.f : linear_unscale(base[tok]), bias, a.vec_y, a.vec_r);
     }
   };
 #pragma unroll 1
@@ -627,10 +684,9 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
 }
 
 template <typename T, int K, typename S, int GS, bool VEC>
-static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, hipStream_t stream) {
+static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, const uint32_t* base, hipStream_t stream) {
   BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, GS, VEC>>(S::kLds)));
-  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, GS, VEC>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles,
-                     static_cast<const char*>(a.ws));
+  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, GS, VEC>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles, base);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
@@ -638,18 +694,23 @@ static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, hipSt
 template <typename T, int K, typename S>
 static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
   const int images = bpdq_ceil_div(a.d_in, 256) * 4, blocks = bpdq_ceil_div(a.n_tok, S::kToks) * (S::kToks / 32);
-  hipLaunchKernelGGL((linear_order_kernel<T>), dim3(bpdq_ceil_div(images * blocks, 4)), dim3(256), 0, stream, a, images * blocks, images,
-                     static_cast<u32x4_t*>(a.ws));
+  // behind the images
+  uint32_t* base = reinterpret_cast<uint32_t*>(static_cast<char*>(a.ws) + linear_image_bytes(a.n_tok, a.d_in));
+  if constexpr (!__is_same(T, _Float16)) {
+    hipLaunchKernelGGL((linear_base_kernel<T>), dim3(bpdq_ceil_div(a.n_tok, 4)), dim3(256), 0, stream, a, base);
+    BPDQ_LAUNCH_CHECK();
+  }
+  hipLaunchKernelGGL((linear_order_kernel<T>), dim3(bpdq_ceil_div(images * blocks, 4)), dim3(256), 0, stream, a, images * blocks, images, base);
   BPDQ_LAUNCH_CHECK();
   const int tok_tiles = bpdq_ceil_div(a.n_tok, S::kToks);
   const dim3 grid(bpdq_ceil_div(a.d_out, S::kRows) * tok_tiles);
   const int wpg = a.group / 32;
   if (a.vec_w) {
-    if (wpg % 4 == 0) return linear_launch_as<T, K, S, 4, true>(a, grid, tok_tiles, stream);
-    if (wpg % 2 == 0) return linear_launch_as<T, K, S, 2, true>(a, grid, tok_tiles, stream);
-    return linear_launch_as<T, K, S, 1, true>(a, grid, tok_tiles, stream);
+    if (wpg % 4 == 0) return linear_launch_as<T, K, S, 4, true>(a, grid, tok_tiles, base, stream);
+    if (wpg % 2 == 0) return linear_launch_as<T, K, S, 2, true>(a, grid, tok_tiles, base, stream);
+    return linear_launch_as<T, K, S, 1, true>(a, grid, tok_tiles, base, stream);
   }
-  return linear_launch_as<T, K, S, 1, false>(a, grid, tok_tiles, stream);
+  return linear_launch_as<T, K, S, 1, false>(a, grid, tok_tiles, base, stream);
 }
 
 template <typename T, int K, int R, int NT>

@@ -5,7 +5,7 @@ using namespace bpdq;
 
 extern "C" size_t bpdq_linear_workspace_bytes(int n_tok, int d_in) {
   if (n_tok <= kLinRowsMost || d_in <= 0 || d_in % 32) return 0;
-  return bpdq_align_up((size_t)n_tok, kLinTokPad) * bpdq_align_up((size_t)d_in, 256) * 2;
+  return linear_image_bytes(n_tok, d_in) + bpdq_align_up((size_t)n_tok, kLinTokPad) * sizeof(uint32_t);
 }
 
 extern "C" int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,

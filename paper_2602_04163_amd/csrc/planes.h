@@ -1,7 +1,7 @@
-// Weights as operands of the 16-bit matrix instructions, straight from the stored bit-plane format (paper Eq. 1).
+// Weights as fp16 operands of the matrix instructions, straight from the stored bit-plane format (paper Eq. 1).
 //
-// A group's 2^k levels of a row, ((C_0 + b_1 C_1) + b_2 C_2) + ... in fp32 in this order, rounded once to the type, lie in
-// registers as two tables of bytes (low and high halves), and v_perm_b32, which picks four bytes out of eight by four
+// A group's 2^k levels of a row, ((C_0 + b_1 C_1) + b_2 C_2) + ... in fp32 in this order, rounded once to fp16 (11 bits; the coefficients
+// are halves themselves, so small sums are exact), lie in registers as two tables of bytes (low and high halves), and v_perm_b32, which picks four bytes out of eight by four
 // selector bytes, turns four codes into four low or high bytes at once.
 //
 // The codes of four columns as bytes come from the plane words by a shift and a mask if the columns are eight apart, so the 32
@@ -17,15 +17,10 @@ namespace bpdq {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
-template <typename T>
-__device__ __forceinline__ uint32_t bits16(float v) {
-  return __builtin_bit_cast(unsigned short, (T)v);
-}
-
 __device__ __forceinline__ uint32_t bit_select(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
 
 // The levels of one (row, group).
-template <typename T, int K>
+template <int K>
 struct PlaneLevels {
   static constexpr int kRegs = K <= 2 ? 1 : 1 << (K - 2);
   uint32_t lo[kRegs], hi[kRegs];
@@ -38,7 +33,7 @@ struct PlaneLevels {
 #pragma unroll
       for (int i = 0; i < K; ++i)
         if (n >> i & 1) s += (float)c[i + 1];
-      v[n] = bits16<T>(s);
+      v[n] = __builtin_bit_cast(unsigned short, (_Float16)s);
     }
 #pragma unroll
     for (int r = 0; r < kRegs; ++r) {
@@ -91,8 +86,7 @@ struct PlaneWord {
     else return first | ((v[1] >> (2 * f)) & (K == 3 ? 0x01010101u : 0x03030303u)) << 2;
   }
   // the eight values of step f
-  template <typename T>
-  __device__ __forceinline__ u32x4_t values(const PlaneLevels<T, K>& levels, int f) const {
+  __device__ __forceinline__ u32x4_t values(const PlaneLevels<K>& levels, int f) const {
     uint32_t a, b, c, d;
     levels.take(codes(even, f), a, b);
     levels.take(codes(odd, f), c, d);

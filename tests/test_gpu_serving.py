@@ -2,9 +2,9 @@
 cache as it is written and read, and attention over it.
 
 Tolerances.  u = 2^-11 (float16) or 2^-8 (bfloat16) is the largest relative error of one rounding to the type, e = 2^-24 that of
-fp32.  Product: What is rounded once (u |What|), a sum of d products in any order costs at most d e, the result is rounded once:
-|error| <= (u + (d + 16) e) S + u |y|, S = sum |What| |x| + |bias|, times the activation's steepest slope (below 1.13), and over all
-values (roundings are independent) at most 2 u of the norm of what was rounded.
+fp32.  Product: What is rounded once to fp16 (w = 2^-11 of it), a sum of d products in any order costs at most d e, the result is
+rounded once: |error| <= (w + (d + 16) e) S + u |y|, S = sum |What| |x| + |bias|, times the activation's steepest slope (below 1.13), and
+over all values (roundings are independent) at most u + w of the norm of what was rounded.
 Attention: scores carry (dim + 16) e times max |scale| sum |q| |k| (plus |log2| terms of the exponential, the same size), probabilities
 an error of u16 = 2^-11 each from their rounding to fp16 (or 2^-25 of the largest), the result u.
 """
@@ -21,7 +21,7 @@ pytestmark = pytest.mark.gpu
 
 TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
-E = 2.0 ** -24
+E, W16 = 2.0 ** -24, 2.0 ** -11
 
 
 @pytest.fixture(scope="module")
@@ -51,12 +51,12 @@ def _on(planes, coefs, dev):
 def _check_linear(y, want, size, kind, d_in, residual=None):
     u = U[kind]
     got = _np(y)
-    tol = 1.13 * (u + (d_in + 16) * E) * size + u * np.abs(want) + 2.0 ** -24 * (1 + d_in)
+    tol = 1.13 * (W16 + (d_in + 16) * E) * size + u * np.abs(want) + 2.0 ** -24 * (1 + d_in)
     if residual is not None:
         tol += E * np.abs(residual)
     assert (np.abs(got - want) <= tol).all(), np.max(np.abs(got - want) / tol)
     base = want if residual is None else np.concatenate([want, want - residual])
-    assert np.linalg.norm(got - want) <= 2 * u * np.linalg.norm(base) + 2.0 ** -20 * np.sqrt(want.size)
+    assert np.linalg.norm(got - want) <= (u + W16) * np.linalg.norm(base) + 2.0 ** -20 * np.sqrt(want.size)
 
 
 @pytest.mark.parametrize("bits,group,d_out,d_in,n,kind,act,bias,residual", [
@@ -142,14 +142,32 @@ def test_linear_keeps_what_is_not_finite_in_its_row(dev, n):
     assert torch.equal(y[keep], clean[keep])
 
 
+@pytest.mark.parametrize("n", [1, 3, 20, 70, 260])
+def test_linear_of_tokens_of_all_sizes(dev, n):
+    """bfloat16 reaches far beyond float16: tokens from 2^-120 to 2^100, each as exact as it would be alone; zeros and denormals."""
+    d_in, d_out = 288, 48
+    planes, coefs = _layer(d_out, d_in, 2, 96, n)
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn((n, d_in), generator=g) * torch.exp(torch.randn(d_in, generator=g))
+    power = torch.linspace(-120, 100, n).round() if n > 1 else torch.tensor([-120.0])
+    x = (x * torch.exp2(power)[:, None]).bfloat16()
+    if n > 3:
+        x[1] = 0
+        x[2] = 1e-39 * torch.randn(d_in, generator=g)
+    want, size = so.linear(planes, coefs, 96, _np(x))
+    y = _np(bq.bpdq_linear(*_on(planes, coefs, dev), 96, x.to(dev)))
+    tol = (W16 + (d_in + 16) * E) * size + U["bf16"] * np.abs(want) + 2.0 ** -29 * np.abs(_np(x)).max(1, keepdims=True) * d_in * 0.3 + 1e-40
+    assert (np.abs(y - want) <= tol).all(), np.max(np.abs(y - want) / tol)
+
+
 def test_linear_is_the_dequantized_product(dev):
-    """Tokens that are unit vectors give the columns of What, rounded."""
+    """Tokens that are unit vectors give the columns of What, rounded to fp16 and then to the type."""
     planes, coefs = _layer(64, 256, 4, 64, 9)
     p, c = _on(planes, coefs, dev)
     w = bq.bpdq_dequant_fp16(p, c, 64)
     for t in (torch.float16, torch.bfloat16):
         y = bq.bpdq_linear(p, c, 64, torch.eye(256, device=dev, dtype=t))
-        assert torch.equal(y, w.t().to(t))
+        assert torch.equal(y, w.t().half().to(t))
 
 
 def test_linear_refuses_tensors(dev):
