@@ -6,7 +6,7 @@
 // a time: lane (row l % 16, quarter l / 16) loads 16 bytes of each plane, its quarter's 128 columns, and is the operand of that row
 // for these columns, whatever the order in which they are contracted.  The partial sums meet in LDS, in the order of the
 // wavefronts.
-// One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 6.9 us (3.8 MB; latency, in one round of 224 work-groups).  16 fp16
+// One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 7.0 us (3.8 MB; latency, in one round of 224 work-groups).  16 fp16
 // tokens, 18944 x 3584 at 3 bits: 15 to 16 us for 30 MB, 1.9 to 2.0 TB/s, vector issue.
 //
 // More tokens: tiles (linear_tiles_kernel), which decode a row's weights once for 64 to 256 tokens.
@@ -116,8 +116,9 @@ constexpr int kLinWaves = kLinThreads / 64;
 
 constexpr int kRowPitch = 512 + 16;                       // bytes of a token's 256 columns in LDS: 16 tokens fall into all 64 banks
 
+// (Registers for one work-group to a CU: with the 128 of two, 16 rows spill, and 20 fp16 tokens of 11264 columns at 4 bits take 33 us, not 17.)
 template <typename T, int K, int R, int NT>
-__global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear_rows_kernel(LinearArgs a) {
+__global__ __launch_bounds__(kLinThreads, 2) void linear_rows_kernel(LinearArgs a) {
   constexpr int kRows = 16 * R, kToks = 16 * NT;
   constexpr int kStageBytes = kLinWaves * 16 * kRowPitch, kPartBytes = kLinWaves * kToks * kRows * 4;
   __shared__ uint4 lds_raw[(kStageBytes > kPartBytes ? kStageBytes : kPartBytes) / 16];
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
   const int toks = a.n_tok - tok0 < kToks ? a.n_tok - tok0 : kToks;
   char* stage = reinterpret_cast<char*>(lds_raw) + wave * 16 * kRowPitch;
   constexpr bool kScale = !__is_same(T, _Float16);
-  __shared__ uint32_t most_s[kLinWaves][kToks], base_s[kToks];
+  __shared__ uint32_t most_s[kToks > kLinWaves ? kToks : kLinWaves], base_s[kToks];
 
   f32x4_t acc[R][NT];
 #pragma unroll
@@ -138,7 +139,8 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
   // the next row tile's words and first coefficients, requested a tile ahead
   typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
   u32x2_t w_next[K];
-  _Float16 c_next[K + 1];
+  _Float16 c_next[K + 1], c_next2[K + 1];                // of the first word and, where groups have an odd number of words, the second
+  const bool odd = wpg % 2 != 0;
   auto row = [&](int r) { return row0 + 16 * r + low < a.d_out ? row0 + 16 * r + low : a.d_out - 1; };
   auto load_c = [&](int r, int word, _Float16 (&c)[K + 1]) {
     const _Float16* p = a.coefs + (long)row(r) * n_grp + (word < nw ? word : 0) / wpg;
@@ -157,32 +159,32 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
       }
     }
     load_c(r, word, c_next);
+    if (odd) load_c(r, word + 1, c_next2);
   };
   if (8 * wave < nw) load_w(0, 8 * wave + 2 * quarter);
   if constexpr (kScale) {                                // (while the first words are on their way)
-    for (int t0 = 0; t0 < toks; t0 += 4) {
-      uint32_t most[4] = {0, 0, 0, 0};
-      for (int c = 8 * tid; c < a.d_in; c += 8 * kLinThreads)
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (t0 + t < toks) most[t] = linear_most(linear_load8(static_cast<const T*>(a.x) + (tok0 + t0 + t) * a.ldx + c, a.vec_x), most[t]);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t0 + t >= toks) break;                       // uniform
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-          const uint32_t b = __shfl_xor(most[t], o, 64);
-          most[t] = most[t] > b ? most[t] : b;
-        }
-        if (lane == 0) most_s[wave][t0 + t] = most[t];
-      }
+    // a power of two of threads to each token, so that all tokens are read at once
+    const int share = 9 - (toks > 1 ? 32 - __builtin_clz(toks - 1) : 0), t = tid >> share;      // as powers of two
+    const int lanes = 1 << share, part = share < 6 ? share : 6;
+    uint32_t most = 0;
+    if (t < toks) {
+      const T* x = static_cast<const T*>(a.x) + (tok0 + t) * a.ldx;
+#pragma unroll 4
+      for (int c = 8 * (tid & (lanes - 1)); c < a.d_in; c += 8 * lanes) most = linear_most(linear_load8(x + c, a.vec_x), most);
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      if (o >> part) continue;                           // uniform
+      const uint32_t b = __shfl_xor(most, o, 64);
+      most = most > b ? most : b;
+    }
+    if ((tid & ((1 << part) - 1)) == 0) most_s[tid >> part] = most;
     __syncthreads();
     if (tid < toks) {
-      uint32_t most = 0;
-#pragma unroll
-      for (int w = 0; w < kLinWaves; ++w) most = most > most_s[w][tid] ? most : most_s[w][tid];
-      base_s[tid] = linear_base(most);
+      const int n = lanes >> part;
+      uint32_t all = 0;
+      for (int w = 0; w < n; ++w) all = all > most_s[tid * n + w] ? all : most_s[tid * n + w];
+      base_s[tid] = linear_base(all);
     }
     __syncthreads();
   }
@@ -234,18 +236,16 @@ __global__ __launch_bounds__(kLinThreads, NT == 1 && R == 1 ? 4 : 2) void linear
       for (int i = 0; i < K; ++i) w[i] = w_next[i];
 #pragma unroll
       for (int i = 0; i <= K; ++i) c[i] = word < nw ? c_next[i] : (_Float16)0.f;      // words past the end add nothing
+      _Float16 c2[K + 1];
+#pragma unroll
+      for (int i = 0; i <= K; ++i) c2[i] = word + 1 < nw && odd ? c_next2[i] : (_Float16)0.f;
       if (r + 1 < R) load_w(r + 1, word);
       else if (w0 + 8 * kLinWaves < nw) load_w(0, word + 8 * kLinWaves);
       PlaneLevels<K> levels;
       levels.set(c);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        if (j == 1 && wpg % 2 != 0) {                    // uniform: the second word may be another group's
-          load_c(r, word + 1, c);
-#pragma unroll
-          for (int i = 0; i <= K; ++i) c[i] = word + 1 < nw ? c[i] : (_Float16)0.f;
-          levels.set(c);
-        }
+        if (j == 1 && odd) levels.set(c2);               // uniform: the second word may be another group's
         uint32_t words[K];
 #pragma unroll
         for (int i = 0; i < K; ++i) words[i] = w[i][j];
