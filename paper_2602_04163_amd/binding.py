@@ -441,7 +441,8 @@ ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 def _rows(t, dtype, shape, name):
-    """The row stride of a tensor of the given shape on the GPU whose rows (all axes but the first) are dense."""
+    """The row stride of a tensor of the given shape on the GPU whose rows (all axes but the first) are dense and do not overlap (one row that
+    is expanded to several does)."""
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise BpdqError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
     strides = t.stride()
@@ -450,7 +451,11 @@ def _rows(t, dtype, shape, name):
         if strides[axis] != step and shape[axis] > 1:
             raise BpdqError(f"{name}: its rows must be dense")
         step *= shape[axis]
-    return max(strides[0], step) if shape[0] > 1 else step
+    if shape[0] <= 1:
+        return step
+    if strides[0] < step:
+        raise BpdqError(f"{name}: its rows must not overlap")
+    return strides[0]
 
 
 def _call(name, rc):
