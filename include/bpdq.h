@@ -320,11 +320,11 @@ int bpdq_kv_read(const bpdq_kv_cache* cache /* host */, const int* page_table, i
  *   max_q, max_kv : at least the largest count of queries and of cached tokens of a sequence; the work is laid out by them,
  *   and longer sequences are cut to them.  max_kv <= max_pages * page.
  * Scores and sums are fp32 on exact products (Q in bf16 is scaled by a power of two per row and head and taken as fp16, where a value
- * below 2^-31 of the row's largest may lose bits); the unnormalised probabilities are rounded to fp16 for the product with V,
- * with 11 bits where they are above 2^-14 of the row's maximum so far (for max_q * n_q / n_kv <= 32) or above 2^-11 of it (for more; there
- * they are taken relative to a reference within 2^8 of that maximum and with the page's scale of V in them), fewer below; out is rounded
+ * below 2^-31 of the row's largest may lose bits); the unnormalised probabilities are rounded to fp16 for the product with V: for
+ * max_q * n_q / n_kv <= 32 with 11 bits where they are above 2^-14 of the row's maximum so far, for more rows times their page's scale of V,
+ * with 11 bits where that product is above 2^-21 of the row's largest so far, and with fewer below; out is rounded
  * once.  A call's result does not change from run to run; the split of long caches depends on n_seq,
- * max_q, n_q, n_kv, head_dim, max_kv and window alone.
+ * max_q, n_q, n_kv, head_dim, max_kv and window alone.  The cache's scales must not be negative (bpdq_kv_write's are not).
  * Pages outside [0, n_pages) count as not visible.
  * Requirements: n_seq <= 65535; max_q * (n_q / n_kv) <= 2^24; ws 256-byte aligned, of bpdq_kv_attention_workspace_bytes() bytes
  * (0 where nothing is split, ws may be NULL then).  out must not overlap Q.

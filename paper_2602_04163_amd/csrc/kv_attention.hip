@@ -361,10 +361,14 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
 // 4096 bf16 tokens, 28 heads of 128 on 4 key heads, causal: 150 to 159 us, 760 to 800 TFLOP/s (a library product reaches 1450; the matrix
 // instructions of the same work take 44 % of the time, and the exponentials beside them share the SIMD's issue).
 // What bounds it is the vector unit, so the softmax is kept to a multiply-add, an exponential, a maximum, a sum and half a conversion per score:
-//  - the running maximum is followed lazily: sums are rescaled only when a row's scores grow by more than 2^8, so probabilities are up to 2^8
-//    relative to the reference and are held as 2^7 times that (fp16 reaches 2^16; what lies below 2^-21 of the reference becomes denormal);
-//  - the scale of V goes into the exponent, relative to a reference v_ref that changes when it is exceeded or undershot by 2^10, so P V adds up
-//    in the accumulators; the row's sum takes it out again, once per tile.
+//  - running maxima are followed lazily: sums are rescaled only when a row's terms grow by more than 2^8 of the reference;
+//  - the scale of V goes into the exponent, so P V adds up in the accumulators.  A row has two references for that: m, the largest z, for the sum of
+//    its p, and mv, the largest z + log2(scale of V), for its sums of p v.  The terms of the product are 2^7 exp2(z + log2(scale) - mv): up
+//    to 2^15 of fp16's 2^16, and denormal, with an absolute error, below 2^-21 of the largest p scale of the tokens that the row sees.  One factor per
+//    tile, undo, turns a tile's sum of these terms into its share of l.  Both references are of what the row itself sees, and only ever rise, so
+//    scales of V however far apart neither overflow a sum nor hide another page's terms: what is lost is small beside the row's largest term.
+//    (Where a tile's scale is so small that its terms would leave the range of fp32, below 2^-57, they are held at that: the product takes
+//    zeros, which is what they are in fp16, and l its whole share.)
 // The scale of scores must not be negative for the maximum: its sign goes into Q.
 template <typename T, int D>
 struct AttnPrompt {
@@ -515,7 +519,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   float m = -__builtin_huge_valf(), l = 0.f;             // reference and sum of the lane's row (half of its tokens)
-  float v_ref = 0.f, v_inv = __builtin_huge_valf();
+  float mv = -__builtin_huge_valf();                     // reference of the row's sums of p v
   // Operands from LDS come kG at a time, a group ahead of their products; the barriers for the scheduler keep it so.
   constexpr int kG = kDt > 2 ? kDt / 2 : kDt, kGroups = 4 * kDt / kG;
   f16x8_t part[2][kG];
@@ -566,9 +570,9 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
     if (tile + 3 > known + 63) learn(tile);
     const bool there = lane_of(page_of, tile - known) >= 0;
     const float k_scale = lane_of(k_scale_of, tile - known);
-    float v_scale = lane_of(v_scale_of, tile - known);
+    const float v_scale = lane_of(v_scale_of, tile - known);
     const bool bad = !(k_scale < __builtin_huge_valf()) || !(v_scale < __builtin_huge_valf());
-    v_scale = fmaxf(v_scale, 0x1p-120f);                 // (of zeros: the exponent wants a logarithm)
+    const float log_v = bad ? 0.f : __builtin_amdgcn_logf(fmaxf(v_scale, 0x1p-120f));
     float f = k_scale * q_scale;
     // scores of register e of half u: token t0 + 32 u + 16 (e / 8) + 8 half + e % 8
     if (t0 < all_lo || t0 + kKvTile > all_hi || bad || !there) {        // uniform
@@ -588,32 +592,21 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(s[0][e], s[1][e]), top);
     top = fmaxf(top, __shfl_xor(top, 32, 64)) * f;
-    if (__any(top > m + 8.f)) {
-      const float m_new = fmaxf(m, top);
-      const float fade = m_new == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+    const float top_v = top + log_v;
+    if (__any(top > m + 8.f || top_v > mv + 8.f)) {
+      const float m_new = fmaxf(m, top), mv_new = fmaxf(mv, top_v);
+      const bool none = m_new == -__builtin_huge_valf(); // so far the row has seen nothing
+      const float fade = none ? 1.f : __builtin_amdgcn_exp2f(m - m_new), fade_v = none ? 1.f : __builtin_amdgcn_exp2f(mv - mv_new);
       m = m_new;
+      mv = mv_new;
       l *= fade;
 #pragma unroll
       for (int d = 0; d < kDt; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] *= fade;
+        for (int e = 0; e < 16; ++e) o[d][e] *= fade_v;
     }
-    float ratio = bad ? 1.f : v_scale * v_inv;
-    if (!bad && !(ratio <= 1.f && ratio >= 0x1p-10f)) {  // uniform
-      // 2^64 bounds the sums: what was added under a scale that much larger stays what counts
-      const float ref = 2.f * v_scale, by = v_ref / ref;
-      if (by < 0x1p64f) {
-#pragma unroll
-        for (int d = 0; d < kDt; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= by;
-        v_ref = ref;
-        v_inv = 1.f / ref;
-      }
-      ratio = v_scale * v_inv;
-    }
-    const float shift = 7.f + __builtin_amdgcn_logf(ratio), undo = __builtin_amdgcn_exp2f(-shift);
-    const float base = m == -__builtin_huge_valf() ? shift : shift - m;
+    const bool none = m == -__builtin_huge_valf();
+    const float base = none ? 0.f : fmaxf(log_v + (m - mv) + 7.f, -57.f) - m;
     __builtin_amdgcn_sched_barrier(0);
 
     // the next tile's scores beside this one's exponentials
@@ -632,6 +625,7 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    const float undo = none ? 1.f : __builtin_amdgcn_exp2f(-(base + m));
     l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undo, l);
     // K two tiles ahead and V one are made beside its products
 #pragma unroll
@@ -656,7 +650,8 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
   }
   l += __shfl_xor(l, 32, 64);
   if (!on) return;
-  const float back = v_ref * 0x1p-7f;                    // of the sums
+  // of the sums, to the units of l
+  const float back = m == -__builtin_huge_valf() ? 1.f : __builtin_amdgcn_exp2f(mv - m - 7.f);
   // a block's channels 8 q + 4 half + j
   if (n_chunk > 1) {
     const long slot = (((long)seq * a.q_tiles + q_tile) * a.c.n_kv + h) * a.n_chunk + chunk;
