@@ -24,8 +24,8 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kLinRowsMost = 32;                           // tokens of the kernel without an ordering of X
 constexpr int kLinTokPad = 256;                           // the ordering covers whole tiles of any shape
 
-static inline size_t linear_image_bytes(int n_tok, int d_in) {
-  return bpdq_align_up((size_t)n_tok, kLinTokPad) * bpdq_align_up((size_t)d_in, 256) * 2;
+static inline size_t linear_image_bytes(int n_tok, int d_in) {         // with an image of zeros to a block of 32 tokens
+  return bpdq_align_up((size_t)n_tok, kLinTokPad) * (bpdq_align_up((size_t)d_in, 256) * 2 + 128);
 }
 
 struct LinearArgs {
@@ -319,7 +319,8 @@ struct LinearTile {
 
 // X in the order of the tile kernel: images of 32 tokens x 64 columns, [token / 32][chunk of 256 columns][j][4 KB], of words j and 4 + j of the
 // chunk (half 0 and 1).  The operand of (token t, half h, step f), 16 bytes, lies at 128 t + 16 ((4 h + f) ^ (t / 2 & 7)): 16 consecutive tokens
-// of a step and half fall into all 64 banks of LDS.  Tokens from n_tok on and columns from d_in on are zero.
+// of a step and half fall into all 64 banks of LDS.  Tokens from n_tok on and columns from d_in on are zero (a block's images may go on behind the
+// last chunk).
 // One wavefront per image.
 template <typename T>
 __global__ __launch_bounds__(256) void linear_order_kernel(LinearArgs a, int n_image, int images, const uint32_t* __restrict__ base) {
@@ -429,8 +430,9 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int all_chunks = bpdq_ceil_div(nw, 2 * W);
   const int n_chunk = bpdq_ceil_div(all_chunks, S::KS);  // of a part, the last one maybe past the end
 
-  // a stage: kToks / 32 images; the wavefront requests kDma runs of 1 KB.  Stages past the end repeat the last one.
-  const int n_image = 4 * all_chunks;
+  // a stage: kToks / 32 images; the wavefront requests kDma runs of 1 KB.  Stages past the end take the last image, which is of zeros where a
+  // part may come to multiply it: under levels of zero an infinity would become a NaN.
+  const int n_image = 4 * all_chunks + (S::KS > 1);
   const char* x_from = static_cast<const char*>(a.ws) + (long)(tok0 / 32) * n_image * 4096;
   unsigned run_from[S::kDma];                            // of a run, in bytes from x_from (all of a tile within 32 bits)
 #pragma unroll
@@ -702,7 +704,7 @@ static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, const
 
 template <typename T, int K, typename S>
 static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
-  const int images = bpdq_ceil_div(a.d_in, 256) * 4, blocks = bpdq_ceil_div(a.n_tok, S::kToks) * (S::kToks / 32);
+  const int images = bpdq_ceil_div(a.d_in, 256) * 4 + (S::KS > 1), blocks = bpdq_ceil_div(a.n_tok, S::kToks) * (S::kToks / 32);
   // behind the images
   uint32_t* base = reinterpret_cast<uint32_t*>(static_cast<char*>(a.ws) + linear_image_bytes(a.n_tok, a.d_in));
   if constexpr (!__is_same(T, _Float16)) {
