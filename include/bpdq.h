@@ -236,7 +236,8 @@ int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_
  * from the stored planes and coefficients.
  *   X : n_tok x d_in, row stride ldx;  bias : d_out or NULL;  residual : n_tok x d_out, row stride ldr, or NULL;
  *   Y : n_tok x d_out, row stride ldy.  All of one type, BPDQ_F16 or BPDQ_BF16 (uint16 bit patterns); strides in elements.
- *   act : BPDQ_ACT_*; GELU is v Phi(v), GELU_TANH its approximation by tanh, SILU v / (1 + exp(-v)).
+ *   act : BPDQ_ACT_*; GELU is v Phi(v), GELU_TANH its approximation by tanh, SILU v / (1 + exp(-v)), each in fp32 with a relative error below
+ *   2^-16, and 2^-21 of the exponential's argument where that is larger.
  * What is evaluated in fp32 and rounded once to fp16; X in bf16 is scaled by a power of two per token and taken as fp16, which changes no
  * value above 2^-29 of the token's largest; the products are exact, sums, bias, activation and residual fp32; Y is rounded once.
  * (A level of a row beyond 65504 becomes infinite.)  A NaN or infinity in a row of X reaches that row of Y alone.
