@@ -153,6 +153,15 @@ def _workspace(nbytes, device):
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _ws(ws):
+    """Address and bytes of a workspace, which may be a caller's: a contiguous tensor of any type on the GPU, or None."""
+    if ws is None:
+        return None, 0
+    if not (ws.is_cuda and ws.is_contiguous()):
+        raise BpdqError("ws: expected a contiguous tensor on the GPU")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def bpdq_version() -> int:
     return load().bpdq_version()
 
@@ -174,7 +183,7 @@ def bpdq_hessian_accumulate(Xc, H, scale=2.0, symmetrize=False, ws=None, _entry=
     if ws is None:
         ws = _workspace(lib.bpdq_hessian_workspace_bytes(n_tok, d_in), H.device)
     rc = getattr(lib, _entry)(_ptr(Xc), n_tok, d_in, Xc.stride(0) if n_tok > 1 else d_in,
-                              scale, _ptr(H), int(bool(symmetrize)), _ptr(ws), ws.numel(),
+                              scale, _ptr(H), int(bool(symmetrize)), *_ws(ws),
                               _stream())
     _check(rc, _entry)
     return H
@@ -206,7 +215,7 @@ def bpdq_hessian_accumulate_timed(kernel, Xc, H, scale=2.0, symmetrize=False, ws
     ev = [ctypes.c_void_p(0 if e is None else e.cuda_event) for e in (ev_begin, ev_end)]
     rc = lib.bpdq_hessian_accumulate_timed(HESSIAN_KERNELS[kernel], _ptr(Xc), n_tok, d_in,
                                            Xc.stride(0) if n_tok > 1 else d_in, scale, _ptr(H),
-                                           int(bool(symmetrize)), _ptr(ws), ws.numel(), _stream(), ev[0], ev[1])
+                                           int(bool(symmetrize)), *_ws(ws), _stream(), ev[0], ev[1])
     _check(rc, "bpdq_hessian_accumulate_timed")
     return H
 
@@ -227,8 +236,7 @@ def bpdq_prepare(H, damp=0.01, U=None, ws=None):
     info = torch.empty(1, dtype=torch.int32, device=H.device)
     if ws is None:
         ws = _workspace(lib.bpdq_prepare_workspace_bytes(d_in), H.device)
-    rc = lib.bpdq_prepare(_ptr(H), d_in, damp, _ptr(U), _ptr(dead), _ptr(info), _ptr(ws),
-                          ws.numel(), _stream())
+    rc = lib.bpdq_prepare(_ptr(H), d_in, damp, _ptr(U), _ptr(dead), _ptr(info), *_ws(ws), _stream())
     _check(rc, "bpdq_prepare")
     return U, dead, info
 
@@ -268,7 +276,7 @@ def bpdq_quantize_layer(W, U, dead, params: BpdqParams, want_w_hat=True, ws=None
         ws = _workspace(need, dev)
     rc = lib.bpdq_quantize_layer(_ptr(W), d_out, d_in, _ptr(U), _ptr(dead), ctypes.byref(params),
                                  _ptr(out["planes"]), _ptr(out["coefs"]), _ptr(out["W_hat"]),
-                                 _ptr(out["grp_err"]), _ptr(out["grp_iter"]), _ptr(ws), ws.numel(),
+                                 _ptr(out["grp_err"]), _ptr(out["grp_iter"]), *_ws(ws),
                                  _stream())
     _check(rc, "bpdq_quantize_layer")
     return out
@@ -300,7 +308,7 @@ def bpdq_quantize_layers(W, seg_end, U, dead, params: BpdqParams, want_w_hat=Tru
     rc = lib.bpdq_quantize_layers(_ptr(W), d_out, d_in, _ptr(U), _ptr(dead), ctypes.byref(params),
                                   n_seg, seg, _ptr(out["planes"]), _ptr(out["coefs"]),
                                   _ptr(out["W_hat"]), _ptr(out["grp_err"]), _ptr(out["grp_iter"]),
-                                  _ptr(ws), ws.numel(), _stream())
+                                  *_ws(ws), _stream())
     _check(rc, "bpdq_quantize_layers")
     return out
 
@@ -370,7 +378,7 @@ def bpdq_channel_order(H, group_size=1):
     d_in = H.shape[0]
     perm = torch.empty(d_in, dtype=torch.int32, device=H.device)
     ws = _workspace(lib.bpdq_channel_order_workspace_bytes(d_in), H.device)
-    _check(lib.bpdq_channel_order(_ptr(H), d_in, group_size, _ptr(perm), _ptr(ws), ws.numel(),
+    _check(lib.bpdq_channel_order(_ptr(H), d_in, group_size, _ptr(perm), *_ws(ws),
                                   _stream()), "bpdq_channel_order")
     return perm
 
@@ -503,7 +511,7 @@ def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None,
     _call("bpdq_linear", lib.bpdq_linear(
         planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx, DTYPES[dtype],
         None if bias is None else bias.data_ptr(), code, None if residual is None else residual.data_ptr(), ldr, Y.data_ptr(), ldy,
-        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream()))
+        *_ws(ws), _stream()))
     return Y
 
 
@@ -613,8 +621,7 @@ def bpdq_kv_attention(cache, page_table, kv_len, q_start, Q, max_q=None, max_kv=
     _call("bpdq_kv_attention", lib.bpdq_kv_attention(
         cache._ref, page_table.data_ptr(), max_pages, n_seq, kv_len.data_ptr(), q_start.data_ptr(), n_tok, max_q, max_kv,
         Q.data_ptr(), ldq, n_q, DTYPES[dtype], dim ** -0.5 if scale is None else scale, 1 if causal else 0, window,
-        out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
-        0 if ws is None else ws.numel(), _stream()))
+        out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), *_ws(ws), _stream()))
     return out
 
 

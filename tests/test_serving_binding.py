@@ -100,3 +100,45 @@ def test_the_stride_of_a_single_row_says_nothing():
         assert bq._rows(_with_row_stride((D_IN,), stride, 1), torch.float16, (1, D_IN), "X") == D_IN
     assert bq._rows(_with_row_stride((D_IN,), 5 * D_IN), torch.float16, (N, D_IN), "X") == 5 * D_IN
     assert bq._rows(_with_row_stride((D_IN,), D_IN, 0), torch.float16, (0, D_IN), "X") == D_IN
+
+
+def _linear_ws(ws):
+    bq.bpdq_linear(gpu(torch.zeros((2, D_OUT, 2), dtype=torch.int32)), gpu(torch.zeros((3, D_OUT, 2), dtype=torch.float16)), 32,
+                   gpu(torch.zeros((N, D_IN), dtype=torch.float16)), Y=gpu(torch.zeros((N, D_OUT), dtype=torch.float16)), ws=ws)
+
+
+def _attend_ws(ws):
+    bq.bpdq_kv_attention(_cache(), _ints((1, 1)), _ints(1), _ints(2), _tokens(4), out=_tokens(4), ws=ws)
+
+
+def _square():
+    return gpu(torch.zeros((64, 64)))
+
+
+WITH_WS = {"linear": _linear_ws, "attention": _attend_ws, "prepare": lambda ws: bq.bpdq_prepare(_square(), U=_square(), ws=ws),
+           "hessian": lambda ws: bq.bpdq_hessian_accumulate(_square(), _square(), ws=ws),
+           "layer": lambda ws: bq.bpdq_quantize_layer(_square(), _square(), None, bq.make_params(2, 64, 64, 1), ws=ws),
+           "layers": lambda ws: bq.bpdq_quantize_layers(_square(), [32, 64], _square(), None, bq.make_params(2, 64, 64, 1), ws=ws)}
+
+
+@pytest.mark.parametrize("name", list(WITH_WS))
+def test_a_workspace_lies_on_the_gpu_in_one_piece(monkeypatch, name):
+    """On the host, or with gaps, a caller's workspace is refused; of whatever type, it counts by its bytes."""
+    seen = []
+
+    class Calls:
+        def __getattr__(self, entry):
+            return (lambda *a: 0) if entry.endswith("_workspace_bytes") else lambda *a: seen.append(a) or 0
+
+    monkeypatch.setattr(bq, "_lib", Calls())
+    monkeypatch.setattr(bq, "_stream", lambda: None)
+    for bad in (torch.zeros(4096, dtype=torch.uint8), gpu(torch.zeros(4096, dtype=torch.uint8))[::2],
+                gpu(torch.zeros((64, 64), dtype=torch.uint8)).t()):
+        with pytest.raises(bq.BpdqError, match="ws"):
+            WITH_WS[name](bad)
+    assert not seen
+    for t in (torch.uint8, torch.float32, torch.float64):
+        ws = gpu(torch.zeros(500, dtype=t))
+        WITH_WS[name](ws)
+        at = seen[-1].index(ws.data_ptr())
+        assert seen[-1][at + 1] == 500 * ws.element_size()
