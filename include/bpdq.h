@@ -319,7 +319,7 @@ int bpdq_kv_read(const bpdq_kv_cache* cache /* host */, const int* page_table, i
  *   Q, out : BPDQ_F16 or BPDQ_BF16;  lse : NULL, or n_tok x n_q floats: log of the sum of exp(scale <q, k>), -inf for a query that
  *   sees nothing.
  *   max_q, max_kv : at least the largest count of queries and of cached tokens of a sequence; the work is laid out by them,
- *   and longer sequences are cut to them.  max_kv <= max_pages * page.
+ *   and longer sequences are cut to them.  max_kv <= max_pages * page and 2^30.
  * Scores and sums are fp32 on exact products (Q in bf16 is scaled by a power of two per row and head and taken as fp16, where a value
  * below 2^-31 of the row's largest may lose bits); the unnormalised probabilities are rounded to fp16 for the product with V: for
  * max_q * n_q / n_kv <= 32 with 11 bits where they are above 2^-14 of the row's maximum so far, for more rows times their page's scale of V,

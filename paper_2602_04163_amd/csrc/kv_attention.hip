@@ -29,6 +29,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / 64;
 constexpr int kAttnMostChunks = 512;                     // of a work item
+constexpr int kAttnMostKv = 1 << 30;                     // a position (from -2^24 on) less a window, and a tile's end, are ints
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct AttnArgs {
@@ -823,7 +824,7 @@ static int attn_by_dim(const AttnArgs& a, const AttnPlan& p, int n_seq, hipStrea
 using namespace bpdq;
 
 extern "C" size_t bpdq_kv_attention_workspace_bytes(int n_seq, int max_q, int max_kv, int n_q, int n_kv, int head_dim, int window) {
-  if (n_seq <= 0 || max_q <= 0 || max_kv <= 0 || n_kv <= 0 || n_q <= 0 || n_q % n_kv || window < 0 ||
+  if (n_seq <= 0 || max_q <= 0 || max_kv <= 0 || max_kv > kAttnMostKv || n_kv <= 0 || n_q <= 0 || n_q % n_kv || window < 0 ||
       (head_dim != 64 && head_dim != 128 && head_dim != 256) || (long)max_q * (n_q / n_kv) > (1L << 24))
     return 0;
   return attn_plan(n_seq, max_q, max_kv, n_q, n_kv, head_dim, window).ws_bytes;
@@ -840,7 +841,7 @@ extern "C" int bpdq_kv_attention(const bpdq_kv_cache* cache, const int* page_tab
   if (n_q <= 0 || n_q % cache->n_kv) return -12;
   const int group = n_q / cache->n_kv;
   if (max_q < 0 || (long)max_q * group > (1L << 24)) return -8;
-  if (max_kv < 0 || max_kv > (long)max_pages * cache->page) return -9;
+  if (max_kv < 0 || max_kv > kAttnMostKv || max_kv > (long)max_pages * cache->page) return -9;
   if (dtype != BPDQ_F16 && dtype != BPDQ_BF16) return -13;
   if (!(scale - scale == 0.f)) return -14;
   if (window < 0) return -16;

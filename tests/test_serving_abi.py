@@ -98,3 +98,13 @@ def test_a_split_call_wants_its_workspace(lib):
     for bad in [(0, 1, 64, 8, 2, 128, 0), (1, 0, 64, 8, 2, 128, 0), (1, 1, 0, 8, 2, 128, 0), (1, 1, 65536, 7, 2, 128, 0),
                 (1, 1, 65536, 8, 2, 96, 0), (1, 1, 65536, 8, 2, 128, -1), (1, 1, 65536, 8, 0, 128, 0)]:
         assert lib.bpdq_kv_attention_workspace_bytes(*bad) == 0
+
+
+def test_attention_counts_positions_in_32_bits(lib):
+    """Positions less a window, and the end of the last tile, have to stay within an int: caches end at 2^30 tokens."""
+    wide = {**ATTENTION, "cache": _cache(), "max_pages": 1 << 25, "n_tok": 0}
+    for most, code in [(1 << 30, 0), ((1 << 30) + 1, -9), ((1 << 31) - 1, -9)]:
+        for window in (0, 16, most - 1):
+            assert lib.bpdq_kv_attention(*{**wide, "max_kv": most, "window": window}.values()) == code, (most, window)
+    size = lib.bpdq_kv_attention_workspace_bytes
+    assert size(1, 1, 1 << 30, 8, 2, 128, 0) > 0 and size(1, 1, (1 << 30) + 1, 8, 2, 128, 0) == 0
