@@ -95,3 +95,49 @@ def test_a_barrier_has_its_wait_for_requests(kernels):
                 continue
             assert not ops[i].startswith("s_barrier"), name
             todo += after[i]
+
+
+def _dma(name):
+    """Requests of a wavefront per stage, and stages, from the tile in a kernel's name."""
+    _, wr, wt, _, _, tt, stages = map(int, re.search("LinearTileI" + r"Li(\d+)E" * 7, name).groups())
+    return 32 * tt * wt * 128 // 1024 // (wr * wt), stages
+
+
+def test_a_barrier_waits_for_all_but_the_stages_ahead(kernels):
+    """What stands between a request and the next barrier leaves at most the requests of the stages behind the next one outstanding, and before
+    the loop the first quarter of the last stage's too.  (Other vector memory operations in between make a wait longer, not shorter.)"""
+    for name, ops in kernels.items():
+        per_stage, stages = _dma(name)
+        after = _after(ops)
+
+        def walk(limit):
+            """Barriers that a request reaches without a wait for all but `limit` in between."""
+            todo, done, reached = [j for i, op in enumerate(ops) if "load_lds" in op for j in after[i]], set(), set()
+            while todo:
+                i = todo.pop()
+                if i in done:
+                    continue
+                done.add(i)
+                count = re.search(r"vmcnt\((\d+)\)", ops[i]) if ops[i].startswith("s_waitcnt") else None
+                if count and int(count.group(1)) <= limit:
+                    continue
+                if ops[i].startswith("s_barrier"):
+                    reached.add(i)
+                    continue
+                todo += after[i]
+            return reached
+
+        def repeats(i):
+            todo, done = list(after[i]), set()
+            while todo:
+                j = todo.pop()
+                if j in done:
+                    continue
+                done.add(j)
+                todo += after[j]
+            return i in done
+
+        ahead = (stages - 2) * per_stage
+        loop = [i for i, op in enumerate(ops) if op.startswith("s_barrier") and repeats(i)]
+        assert loop and not walk(ahead + per_stage // 4), name
+        assert not walk(ahead) & set(loop), name
