@@ -2,8 +2,8 @@
 // The weights become operands of the 16-bit matrix instructions in registers (planes.h); they are never written anywhere.
 //
 // Few tokens: what bounds it is the planes' way from memory (k / 8 bytes per weight) and the vector instructions that turn
-// codes into values.  A work-group of eight wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 512 at
-// a time: lane (row l % 16, quarter l / 16) loads 16 bytes of each plane, its quarter's 128 columns, and is the operand of that row
+// codes into values.  A work-group of eight wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 256 at
+// a time: lane (row l % 16, quarter l / 16) loads 8 bytes of each plane, its quarter's 64 columns, and is the operand of that row
 // for these columns, whatever the order in which they are contracted.  The partial sums meet in LDS, in the order of the
 // wavefronts.
 // One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 7.0 us (3.8 MB; latency, in one round of 224 work-groups).  16 fp16
@@ -319,6 +319,7 @@ struct LinearTile {
   static constexpr int kRing = kStages * KS * kStage;
   static constexpr size_t kLds = (size_t)kRing + 2 * KS * kTable;
   static_assert(kDma % 4 == 0, "a quarter with each step");
+  static_assert(kStages >= 3, "the requests of a stage are spread over the one before");
   static_assert(kLds <= 160 * 1024, "one work-group to a CU");
   static_assert(KS == 1 || (size_t)(KS / 2) * kRows * kToks * 4 <= kLds, "the joining of the parts has to fit");
 };
@@ -446,8 +447,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     const int run = wave * S::kDma + i;
     run_from[i] = (unsigned)(run / 4) * (unsigned)n_image * 4096u + (unsigned)(run % 4) * 1024u;
   }
-  // A quarter of a stage's runs: requests in one burst hold the wavefront up.  (Two stages leave no time for that.)  Stage of this part: chunk stage / 4, word stage % 4.
-  constexpr bool kBurst = S::kStages == 2;
+  // A quarter of a stage's runs: requests in one burst hold the wavefront up.  Stage of this part: chunk stage / 4, word stage % 4.
   auto request = [&](int stage, int ring, int quarter) {
     int at = (stage / W * S::KS + part) * W + stage % W;
     at = at < n_image ? at : n_image - 1;
@@ -570,14 +570,14 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
 #pragma unroll
   for (int s = 0; s < S::kStages; ++s)
 #pragma unroll
-    for (int q = 0; q < (kBurst || s < S::kStages - 1 ? 4 : 1); ++q) request(s, s, q);
+    for (int q = 0; q < (s < S::kStages - 1 ? 4 : 1); ++q) request(s, s, q);
   load_w(part);
   load_levels(0);
   store_levels(0);
   load_levels(GS);
   take_w();
   if (S::kAcc <= 64) load_w(part + S::KS);
-  wait_vm<(S::kStages - 2) * S::kDma + (kBurst ? S::kDma : S::kDma / 4)>();
+  wait_vm<(S::kStages - 2) * S::kDma + S::kDma / 4>();
   __syncthreads();
   read_levels(0);
 #pragma unroll
@@ -603,12 +603,8 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
           if ((j + 1) % GS == 0) read_levels(stage + 1);
         }
         // the slot of the stage before is free behind its barrier
-        if (f == 3) {
-#pragma unroll
-          for (int q = 0; q < (kBurst ? 4 : 1); ++q) request(stage + S::kStages, ring, q);
-        } else if (!kBurst) {
-          request(stage + S::kStages - 1, ring > 0 ? ring - 1 : S::kStages - 1, f + 1);
-        }
+        if (f == 3) request(stage + S::kStages, ring, 0);
+        else request(stage + S::kStages - 1, ring > 0 ? ring - 1 : S::kStages - 1, f + 1);
         decode(f < 3 ? j : (j + 1) % W, (f + 1) & 3);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
