@@ -442,18 +442,14 @@ __global__ __launch_bounds__(kAttnThreads, D == 256 ? 1 : 2) void attn_prompt_ke
   const int at_q = it.kv - it.q_len + i;
   const int see_lo = a.window > 0 ? at_q - a.window + 1 : 0;
   const int see_hi = !on ? 0 : a.causal && at_q + 1 < it.kv ? at_q + 1 : it.kv;
-  // of all the wavefront's rows: tokens that some see, and that all see
-  int any_lo = on ? see_lo : 0x7fffffff, any_hi = see_hi, all_lo = on ? see_lo : 0, all_hi = on ? see_hi : 0x7fffffff;
+  // of all the wavefront's rows: tokens that all see
+  int all_lo = on ? see_lo : 0, all_hi = on ? see_hi : 0x7fffffff;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const int a0 = __shfl_xor(any_lo, o, 64), a1 = __shfl_xor(any_hi, o, 64), a2 = __shfl_xor(all_lo, o, 64), a3 = __shfl_xor(all_hi, o, 64);
-    any_lo = any_lo < a0 ? any_lo : a0;
-    any_hi = any_hi > a1 ? any_hi : a1;
-    all_lo = all_lo > a2 ? all_lo : a2;
-    all_hi = all_hi < a3 ? all_hi : a3;
+    const int lo = __shfl_xor(all_lo, o, 64), hi = __shfl_xor(all_hi, o, 64);
+    all_lo = all_lo > lo ? all_lo : lo;
+    all_hi = all_hi < hi ? all_hi : hi;
   }
-  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
-  any_hi = __builtin_amdgcn_readfirstlane(any_hi);
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_hi = __builtin_amdgcn_readfirstlane(all_hi);
 
