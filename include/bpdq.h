@@ -241,6 +241,7 @@ int bpdq_gemv(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_
  * What is evaluated in fp32 and rounded once to fp16; X in bf16 is scaled by a power of two per token and taken as fp16, which changes no
  * value above 2^-29 of the token's largest; the products are exact, sums, bias, activation and residual fp32; Y is rounded once.
  * (A level of a row beyond 65504 becomes infinite.)  A NaN or infinity in a row of X reaches that row of Y alone.
+ * (For one fp32 token without any of that bpdq_gemv is quicker.)
  * Y may be the residual itself (same address and stride); other overlaps are not allowed.  The result of a token does not
  * depend on the others of the call beyond the choice of kernel by n_tok, which changes the order of sums.
  * From 33 tokens on X is brought into the order of the matrix instructions first, in ws: 256-byte aligned,
@@ -303,7 +304,7 @@ int bpdq_kv_write(const bpdq_kv_cache* cache /* host */, const int* page_table, 
                   const int* pos, const int* tok_start, int n_tok, int max_tok, const void* K, long ldk,
                   const void* V, long ldv, int dtype, void* stream);
 /* The inverse: tokens pos[b] .. of sequence b into rows tok_start[b] .. tok_start[b+1]-1 of K and V, (code - 128) * scale
- * rounded to dtype.  Tokens that bpdq_kv_write would leave out read as zero (rows of a sequence with pos < 0 and rows that no
+ * rounded to dtype (so in fp16 what lies within half a step of 65504 may read as an infinity).  Tokens that bpdq_kv_write would leave out read as zero (rows of a sequence with pos < 0 and rows that no
  * sequence names are left alone).  Arguments and return codes as above. */
 int bpdq_kv_read(const bpdq_kv_cache* cache /* host */, const int* page_table, int max_pages, int n_seq,
                  const int* pos, const int* tok_start, int n_tok, int max_tok, void* K, long ldk, void* V,
@@ -318,7 +319,8 @@ int bpdq_kv_read(const bpdq_kv_cache* cache /* host */, const int* page_table, i
  * without visible tokens, the page's scale.
  *   Q, out : BPDQ_F16 or BPDQ_BF16;  lse : NULL, or n_tok x n_q floats: log of the sum of exp(scale <q, k>), -inf for a query that
  *   sees nothing.
- *   max_q, max_kv : at least the largest count of queries and of cached tokens of a sequence; the work is laid out by them,
+ *   max_q, max_kv : at least the largest count of queries and of cached tokens of a sequence; all sequences are laid out by them (single
+ *   tokens in one call with a long chunk go through the kernel for many rows, their caches unsplit: in a call of their own they are quicker),
  *   and longer sequences are cut to them.  max_kv <= max_pages * page and 2^30.
  * Scores and sums are fp32 on exact products (Q in bf16 is scaled by a power of two per row and head and taken as fp16, where a value
  * below 2^-31 of the row's largest may lose bits); the unnormalised probabilities are rounded to fp16 for the product with V: for

@@ -594,7 +594,8 @@ def bpdq_kv_attention(cache, page_table, kv_len, q_start, Q, max_q=None, max_kv=
                       out=None, lse=None, ws=None):
     """Attention of rows q_start[b] .. q_start[b+1]-1 of Q (n_tok, n_q, head_dim), the last of them at position kv_len[b] - 1, over
     the kv_len[b] cached tokens of sequence b.  max_q, max_kv: at least the largest counts (all rows and all of the table's
-    pages, if they are not given); scale: 1 / sqrt(head_dim) by default; lse: float32 (n_tok, n_q), filled if given."""
+    pages, if they are not given: right, but laid out for one long chunk, which takes 31 single tokens over caches of up to 16384 4.5 times
+    as long); scale: 1 / sqrt(head_dim) by default; lse: float32 (n_tok, n_q), filled if given."""
     lib = _lib or load()
     n_seq, max_pages = _sequences(page_table, kv_len, q_start)
     dtype, dim = Q.dtype, cache.head_dim

@@ -18,7 +18,8 @@
 //
 // What bounds it: single tokens read the cache once, 2 head_dim bytes per token and key head.  131071 fp16 tokens of 8 key heads of 128 (268 MB, 64
 // heads) take 55 us and 6 us for the join (4.9 and 4.4 TB/s; a large copy reaches 5.3), 32 sequences of 1 to 16384 tokens (538 MB) 115 and 9
-// (4.7 and 4.3); 1000 tokens of 4 key heads 11 us, the latency of four tiles in a row in a wavefront.  Prompts: see below.
+// (4.7 and 4.3), and 165 in all with 17 to 32 rows (four or five tokens a sequence); 1000 tokens of 4 key heads 11 us, the latency of four tiles in a
+// row in a wavefront.  Prompts: see below.
 #include "kv_cache.h"
 
 namespace bpdq {
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_rows_kernel(AttnArgs a) {
 // order.  A wavefront owns 32 rows; S^T = K Q^T and O^T = V^T P^T as above (row a of the first product's operand is the token that makes a lane's
 // scores the second one's operand: 16 s + 8 j + 4 h + i <-> token 16 s + 8 h + 4 j + i of 32).
 //
-// 4096 bf16 tokens, 28 heads of 128 on 4 key heads, causal: 150 to 159 us, 760 to 800 TFLOP/s (a library product reaches 1450; the matrix
+// 4096 bf16 tokens, 28 heads of 128 on 4 key heads, causal: 150 to 164 us, 735 to 800 TFLOP/s (a library product reaches 1450; the matrix
 // instructions of the same work take 44 % of the time, and the exponentials beside them share the SIMD's issue).
 // What bounds it is the vector unit, so the softmax is kept to a multiply-add, an exponential, a maximum, a sum and half a conversion per score:
 //  - running maxima are followed lazily: sums are rescaled only when a row's terms grow by more than 2^8 of the reference;
@@ -771,7 +772,7 @@ static AttnPlan attn_plan(int n_seq, int max_q, int max_kv, int n_q, int n_kv, i
   // kAttnGroups work-groups; a chunk has at least a tile for each wavefront, or four where there are enough work items to begin with.
   // (Measured: 32 sequences of 1 to 16384 tokens, 8 key heads, 146 us with 1024 work-groups, 128 with 1536, 138 with 2048.)  Up to 16 tiles
   // the second launch and its workspace cost more than they save: 1000 tokens, 4 key heads 9.8 us of the GPU in two launches, 11.0 in
-  // one, but 3.5 us less of the host; 1500 tokens 9.8 and 14.5.
+  // one, but 3.5 us less of the host; 1500 tokens 9.8 and 14.5.  (So a replayed graph, without the host, loses 1.2 us by it.)
   const long items = (long)n_seq * n_kv * p.q_tiles;
   const int least = items >= 256 ? 4 * kAttnWaves : kAttnWaves;
   long n = ((p.rows == 128 ? kAttnPromptGroups : kAttnGroups) + items - 1) / items;

@@ -1,13 +1,14 @@
 // Y = act(X What^T + bias) + residual from the stored bit-plane format (paper Eq. 1; Sec. 5 discusses serving).
 // The weights become operands of the 16-bit matrix instructions in registers (planes.h); they are never written anywhere.
 //
-// Few tokens: what bounds it is the planes' way from memory (k / 8 bytes per weight) and the vector instructions that turn
-// codes into values.  A work-group of eight wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 256 at
-// a time: lane (row l % 16, quarter l / 16) loads 8 bytes of each plane, its quarter's 64 columns, and is the operand of that row
+// Few tokens: what bounds it is latency, beside the vector instructions that turn codes into values.  A work-group of eight
+// wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 256 at a time: lane (row l % 16, quarter l / 16) loads 8 bytes of each plane, its quarter's 64 columns, and is the operand of that row
 // for these columns, whatever the order in which they are contracted.  The partial sums meet in LDS, in the order of the
 // wavefronts.
-// One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 7.0 us (3.8 MB; latency, in one round of 224 work-groups).  16 fp16
-// tokens, 18944 x 3584 at 3 bits: 15 to 16 us for 30 MB, 1.9 to 2.0 TB/s, vector issue.
+// One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 7.0 to 7.2 us (3.8 MB; one round of 224 work-groups; a pass over the token for its
+// power of two comes first).  16 fp16 tokens, 18944 x 3584 at 3 bits: 15 to 17 us for 30 MB, 1.8 to 2.0 TB/s: vector instructions issue in 55 % of the
+// cycles, matrix instructions in 7 %; two wavefronts to a SIMD, X not requested ahead, and 14 rounds of columns dealt to eight
+// wavefronts leave the rest empty.
 //
 // More tokens: tiles (linear_tiles_kernel), which decode a row's weights once for 64 to 256 tokens.
 #pragma once
@@ -122,7 +123,9 @@ constexpr int kLinWaves = kLinThreads / 64;
 
 constexpr int kRowPitch = 512 + 16;                       // bytes of a token's 256 columns in LDS: 16 tokens fall into all 64 banks
 
-// (Registers for one work-group to a CU: with the 128 of two, 16 rows spill, and 20 fp16 tokens of 11264 columns at 4 bits take 33 us, not 17.)
+// (Registers for one work-group to a CU: with the 128 of two, 16 rows spill, and 20 fp16 tokens of 11264 columns at 4 bits take 33 us, not 17.
+// With all 256 the forms of one row tile have none in scratch; of the others 14 do, 6 to 74 registers: twice 16 tokens with five row tiles but for
+// fp16 at one plane, with three at three and four planes, with two in bf16 at four, and eight row tiles at four.)
 template <typename T, int K, int R, int NT>
 __global__ __launch_bounds__(kLinThreads, 2) void linear_rows_kernel(LinearArgs a) {
   constexpr int kRows = 16 * R, kToks = 16 * NT;
@@ -411,8 +414,9 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
 
 // Y tile of a work-group of wavefronts that share X.  What bounds it: the vector instructions that decode the weights, beside the matrix instructions, which share a SIMD's issue
 // (a stage takes about the longer of the two and 0.4 of the shorter), and the last round of tiles.  4096 bf16 tokens, 18944 x 3584 at 2 bits:
-// 517 to 590 us from card to card, 0.94 to 1.08 PFLOP/s (a library product of the dense 16-bit weights takes 500); 333 tokens,
-// 8192 x 8192: 100 us, 0.45 PFLOP/s (192 work-groups of 128 x 128 on 256 CUs).
+// 517 to 612 us from card to card, some 50 of it GELU, 0.91 to 1.08 PFLOP/s (a library product of the dense 16-bit weights takes 500); 333 tokens,
+// 8192 x 8192: 100 us, 0.45 PFLOP/s (192 work-groups of 128 x 128 on 256 CUs, a wavefront to a SIMD: matrix instructions take 33 % of the busy
+// cycles, vector ones 24 %, and one does not hide the other's latency).
 //
 // GS: words after which a lane's group may change (of the four that it has of a chunk), VEC: the planes go by 16 bytes.
 //
