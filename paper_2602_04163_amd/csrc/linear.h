@@ -2,9 +2,9 @@
 // The weights become operands of the 16-bit matrix instructions in registers (planes.h); they are never written anywhere.
 //
 // Few tokens: what bounds it is latency, beside the vector instructions that turn codes into values.  A work-group of eight
-// wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 256 at a time: lane (row l % 16, quarter l / 16) loads 8 bytes of each plane, its quarter's 64 columns, and is the operand of that row
-// for these columns, whatever the order in which they are contracted.  The partial sums meet in LDS, in the order of the
-// wavefronts.
+// wavefronts owns 16 R rows and NT tiles of 16 tokens; its wavefronts split the columns, 256 at a time: lane (row l % 16,
+// quarter l / 16) loads 8 bytes of each plane, its quarter's 64 columns, and is the operand of that row for these columns,
+// whatever the order in which they are contracted.  The partial sums meet in LDS, in the order of the wavefronts.
 // One bf16 token, 3584 x 3584 at 2 bits in groups of 128: 7.0 to 7.2 us (3.8 MB; one round of 224 work-groups; a pass over the token for its
 // power of two comes first).  16 fp16 tokens, 18944 x 3584 at 3 bits: 15 to 17 us for 30 MB, 1.8 to 2.0 TB/s: vector instructions issue in 55 % of the
 // cycles, matrix instructions in 7 %; two wavefronts to a SIMD, X not requested ahead, and 14 rounds of columns dealt to eight
