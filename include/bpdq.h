@@ -263,6 +263,94 @@ int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int 
                 const void* X, int n_tok, long ldx, int dtype, const void* bias, int act,
                 const void* residual, long ldr, void* Y, long ldy, void* ws, size_t ws_bytes, void* stream);
 
+/* The two projections of a gated feed-forward block in one call:
+ *   Y[t][f] = act( sum_c Wgate[f][c] X[t][c] + bias[f] ) * ( sum_c Wup[f][c] X[t][c] + bias[d_out + f] ),
+ * f < d_out, from two layers stacked by rows (2 d_out rows, gate first), as bpdq_quantize_layers leaves layers that share one input.
+ *   planes : [bits][2 d_out][d_in/32];  coefs_h : [bits+1][2 d_out][d_in/group];  bias : 2 d_out values or NULL;  Y : n_tok x d_out, row stride ldy.
+ * Types, activations, precision, workspace (bpdq_linear_workspace_bytes) and requirements are those of bpdq_linear; neither projection is rounded
+ * before the product.  Y must not overlap X.  A plane (2 d_out x d_in bits) has to be below 4 GiB.
+ * Returns 0, or a negative code naming the argument (-1 planes, -2 coefs_h, -3 d_out, -4 d_in, -5 bits, -6 group, -7 X,
+ * -8 n_tok, -9 ldx, -10 dtype, -11 bias, -12 act, -13 Y, -14 ldy, -15 ws, -16 ws_bytes). */
+int bpdq_gated_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,
+                      const void* X, int n_tok, long ldx, int dtype, const void* bias, int act, void* Y, long ldy,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* ---- serving side: the norm before a product --------------------------------------------------
+ *   S[t] = X[t] + residual[t],    Y[t][c] = S[t][c] / sqrt( mean_c S[t][c]^2 + eps ) * (offset + weight[c])
+ *   X : n_tok x d, row stride ldx, of type dtype (BPDQ_F32, BPDQ_F16 or BPDQ_BF16), and so weight (d values, or NULL: ones, with offset 0 as they are)
+ *   and Y (row stride ldy);  residual : NULL, or n_tok x d, row stride ldr, of type rdtype: dtype or BPDQ_F32;  S : NULL, or the sum in the
+ *   residual's type, row stride lds (only with a residual).
+ * The sum is fp32 and is rounded once for S; Y comes from it unrounded, its squares summed in fp64, the rest fp32, Y rounded once.  A row with a
+ * NaN or an infinity gets NaN (at an infinity) and zeros or NaN elsewhere; other rows do not see it.
+ * S may be the residual or X, and Y may be X (same address, type and stride); other overlaps are not allowed.
+ * Requirements: 1 <= d <= 65536; eps >= 2^-126; offset and eps finite; any alignment of the elements (16 bytes, strides too, is quicker).
+ * n_tok = 0 launches nothing.
+ * Returns 0, or a negative code naming the argument (-1 X, -2 n_tok, -3 d, -4 ldx, -5 dtype, -6 residual, -7 ldr, -8 rdtype, -9 S, -10 lds,
+ * -11 weight, -12 offset, -13 eps, -14 Y, -15 ldy). */
+int bpdq_rms_norm(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype, void* S,
+                  long lds, const void* weight, float offset, float eps, void* Y, long ldy, void* stream);
+/* The same with Y in 8 bits, as it is kept or sent: codes[t][c] = rint(y / scale) in [-127, 127] (row stride ldc), y before any rounding, with one scale
+ * for a row (group = 0) or for each `group` (32, 64, 128 or 256, a divisor of d) of its channels: scales[t][c / group], dense,
+ * max(amax, 2^-96) * (1/127), amax the largest |y| of the group.  A group with a NaN or an infinity gets the scale NaN.
+ * Returns as above (-14 group, -15 codes, -16 ldc, -17 scales). */
+int bpdq_rms_norm_q8(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype, void* S,
+                     long lds, const void* weight, float offset, float eps, int group, int8_t* codes, long ldc, float* scales,
+                     void* stream);
+
+/* ---- serving side: rotary positions ---------------------------------------------------------------
+ * Turns channel pair i of every head of Q and K at position p by the angle p freq[i]:
+ *   (a, b) -> mscale (a cos - b sin, b cos + a sin),   i < rot / 2; channels from rot on are passed on as they are.
+ *   layout : BPDQ_ROTARY_HALF pairs (i, i + rot/2), BPDQ_ROTARY_INTERLEAVED pairs (2i, 2i+1).  inverse != 0 turns back (by -p freq[i]).
+ *   freq : rot / 2 doubles on the GPU, radians per position;  pos, tok_start, n_seq, n_tok, max_tok : as in bpdq_kv_write, the call's next user:
+ *   row tok_start[b] + i is at position pos[b] + i.  Rows of a sequence with pos < 0, and rows that no sequence names, are left alone.
+ *   Q : n_tok rows of n_q heads of head_dim values, row stride ldq, into Q_out (row stride ldqo);  K likewise (n_kv = 0: none).
+ *   dtype : BPDQ_F32, BPDQ_F16 or BPDQ_BF16.  Q_out may be Q and K_out may be K (same stride); other overlaps are not allowed.
+ * The angle is formed in fp64, so far positions are as good as near ones (2^-24 of a turn); the rotation is fp32, rounded once.
+ * Requirements: rot even, 2 <= rot <= head_dim <= 512; n_seq <= 65535; any alignment of the elements.
+ * n_seq = 0, n_tok = 0, max_tok = 0 or no heads launches nothing.
+ * Returns 0, or a negative code naming the argument (-1 freq, -2 rot, -3 layout, -4 mscale, -6 pos, -7 tok_start, -8 n_seq, -9 n_tok,
+ * -10 max_tok, -11 Q, -12 ldq, -13 n_q, -14 K, -15 ldk, -16 n_kv, -17 head_dim, -18 dtype, -19 Q_out, -20 ldqo, -21 K_out, -22 ldko). */
+#define BPDQ_ROTARY_HALF 0
+#define BPDQ_ROTARY_INTERLEAVED 1
+int bpdq_rotary(const double* freq, int rot, int layout, float mscale, int inverse, const int* pos, const int* tok_start,
+                int n_seq, int n_tok, int max_tok, const void* Q, long ldq, int n_q, const void* K, long ldk, int n_kv,
+                int head_dim, int dtype, void* Q_out, long ldqo, void* K_out, long ldko, void* stream);
+/* The frequencies of the usual scalings, on the host: with f_i = base^(-2i/rot),
+ *   PLAIN f_i;  LINEAR f_i / factor;  NTK the base times factor^(rot/(rot-2)) (rot > 2);
+ *   YARN f_i for pairs that make `high` or more turns in `original` positions, f_i / factor for `low` or fewer, and a ramp over the pairs between
+ *   (pairs counted down and up to whole ones), *mscale = 0.1 log(factor) + 1;
+ *   BANDS the same ends with a ramp over the number of turns.
+ * freq : rot / 2 doubles;  mscale : NULL, or the factor for bpdq_rotary (1 but for YARN).  factor >= 1; 0 < low < high.
+ * Returns 0, or a negative code naming the argument (-1 rot, -2 base, -3 scaling, -4 factor, -5 low, -6 high, -7 original, -8 freq). */
+#define BPDQ_ROTARY_PLAIN 0
+#define BPDQ_ROTARY_LINEAR 1
+#define BPDQ_ROTARY_NTK 2
+#define BPDQ_ROTARY_YARN 3
+#define BPDQ_ROTARY_BANDS 4
+int bpdq_rotary_frequencies(int rot, double base, int scaling, double factor, double low, double high, int original,
+                            double* freq /* host */, double* mscale /* host */);
+
+/* ---- serving side: the next token ------------------------------------------------------------------
+ * For each row of logits (n_tok x n_vocab, row stride ldl, of type dtype), with M its largest value, T = temperature and w_i = exp((x_i - M) / T):
+ *   top_k  keeps the k largest values;
+ *   top_p  keeps of these, in descending order, the fewest whose weights add up to at least top_p times theirs in all (one at least);
+ *   min_p  keeps of these what has w_i >= min_p (more than 1 counts as 1);
+ *   token  = the lowest kept index i with  sum_{kept j <= i} w_j  >  u * sum_{kept j} w_j;   prob = w_i over that sum.
+ * Of equal values the lower index comes first.  T must be above 0: any other T (a NaN too) asks for the largest value, prob 1.  top_k <= 0, top_p >= 1 or
+ * NaN and min_p <= 0 or NaN keep all.  u in [0, 1); below (or NaN) counts as 0, from 1 on as the last.
+ *   temperature, top_k, top_p, min_p : n_tok values each, or NULL (T = 1; nobody asks).  u : n_tok floats.
+ *   token : n_tok ints;  prob : NULL or n_tok floats.
+ * A value of minus infinity or NaN is not there; a row where nothing is there gets token -1 and prob 0.  Plus infinities share the row equally.
+ * Weights are counted in units of 2^-43 of the largest (a token below half a unit is never drawn and adds nothing), their sums are exact, and the
+ * result is the same from run to run.
+ * Requirements: n_vocab <= 2^20; ws 256-byte aligned, of bpdq_sample_workspace_bytes() bytes; any alignment of the elements.  n_tok = 0 launches nothing.
+ * Returns 0, or a negative code naming the argument (-1 logits, -2 n_tok, -3 n_vocab, -4 ldl, -5 dtype, -6 temperature, -7 top_k, -8 top_p,
+ * -9 min_p, -10 u, -11 token, -12 prob, -13 ws, -14 ws_bytes). */
+size_t bpdq_sample_workspace_bytes(int n_tok, int n_vocab);
+int bpdq_sample(const void* logits, int n_tok, int n_vocab, long ldl, int dtype, const float* temperature, const int* top_k,
+                const float* top_p, const float* min_p, const float* u, int* token, float* prob, void* ws, size_t ws_bytes,
+                void* stream);
+
 /* ---- serving side: keys and values in 8 bits --------------------------------------------------
  * The cache is in pages of `page` tokens.  A page and key head hold page * head_dim codes of K, as many of V, and one fp32
  * scale of each; a value is (code - 128) * scale, code - 128 in [-127, 127].  Which page holds which tokens of which

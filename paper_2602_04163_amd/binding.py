@@ -25,7 +25,8 @@ EXPORTS = [
     "bpdq_channel_order_workspace_bytes", "bpdq_channel_order", "bpdq_channel_order_noalloc",
     "bpdq_gather_columns",
     "bpdq_scatter_columns", "bpdq_gather_symmetric", "bpdq_gemv",
-    "bpdq_linear_workspace_bytes", "bpdq_linear", "bpdq_kv_write", "bpdq_kv_read", "bpdq_kv_attention_workspace_bytes", "bpdq_kv_attention",
+    "bpdq_linear_workspace_bytes", "bpdq_linear", "bpdq_gated_linear", "bpdq_rms_norm", "bpdq_rms_norm_q8", "bpdq_rotary_frequencies",
+    "bpdq_rotary", "bpdq_sample_workspace_bytes", "bpdq_sample", "bpdq_kv_write", "bpdq_kv_read", "bpdq_kv_attention_workspace_bytes", "bpdq_kv_attention",
     "bpdq_probe_mfma", "bpdq_probe_copy",
 ]
 
@@ -96,6 +97,21 @@ def load():
     lib.bpdq_linear.argtypes = [vp, vp, ci, ci, ci, ci, vp, ci, cl, ci, vp, ci, vp, cl, vp, cl, vp, sz, vp]
     lib.bpdq_linear_workspace_bytes.restype = sz
     lib.bpdq_linear_workspace_bytes.argtypes = [ci, ci]
+    lib.bpdq_gated_linear.restype = ci
+    lib.bpdq_gated_linear.argtypes = [vp, vp, ci, ci, ci, ci, vp, ci, cl, ci, vp, ci, vp, cl, vp, sz, vp]
+    lib.bpdq_rms_norm.restype = ci
+    lib.bpdq_rms_norm.argtypes = [vp, ci, ci, cl, ci, vp, cl, ci, vp, cl, vp, cf, cf, vp, cl, vp]
+    lib.bpdq_rms_norm_q8.restype = ci
+    lib.bpdq_rms_norm_q8.argtypes = [vp, ci, ci, cl, ci, vp, cl, ci, vp, cl, vp, cf, cf, ci, vp, cl, vp, vp]
+    cd = ctypes.c_double
+    lib.bpdq_rotary_frequencies.restype = ci
+    lib.bpdq_rotary_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, ci, vp, vp]
+    lib.bpdq_rotary.restype = ci
+    lib.bpdq_rotary.argtypes = [vp, ci, ci, cf, ci, vp, vp, ci, ci, ci, vp, cl, ci, vp, cl, ci, ci, ci, vp, cl, vp, cl, vp]
+    lib.bpdq_sample_workspace_bytes.restype = sz
+    lib.bpdq_sample_workspace_bytes.argtypes = [ci, ci]
+    lib.bpdq_sample.restype = ci
+    lib.bpdq_sample.argtypes = [vp, ci, ci, cl, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     for name in ("bpdq_kv_write", "bpdq_kv_read"):
         getattr(lib, name).restype = ci
         getattr(lib, name).argtypes = [kv, vp, ci, ci, vp, vp, ci, ci, vp, cl, vp, cl, ci, vp]
@@ -471,6 +487,14 @@ def _call(name, rc):
         _check(rc, name)
 
 
+def _here(*tensors):
+    """Refuses tensors on another GPU than the current one, on whose stream the kernels run."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise BpdqError(f"a tensor on GPU {t.get_device()}, and the current one is {here}")
+
+
 def _scratch(nbytes, device):
     """A workspace, or None where none is asked for."""
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
@@ -513,6 +537,193 @@ def bpdq_linear(planes, coefs_h, group, X, bias=None, act="none", residual=None,
         None if bias is None else bias.data_ptr(), code, None if residual is None else residual.data_ptr(), ldr, Y.data_ptr(), ldy,
         *_ws(ws), _stream()))
     return Y
+
+
+def bpdq_gated_linear(planes, coefs_h, group, X, bias=None, act="silu", Y=None, ws=None):
+    """Y = act(X Wgate^T + bias[:d_out]) * (X Wup^T + bias[d_out:]) from the stored format: two layers stacked by rows, gate first, as
+    bpdq_quantize_layers leaves them (2 d_out rows); X, bias and Y float16 or bfloat16, for any number of tokens."""
+    lib = _lib or load()
+    _dev(planes, torch.int32, "planes")
+    _dev(coefs_h, torch.float16, "coefs_h")
+    bits, rows, nw = planes.shape
+    d_out, d_in, dtype = rows // 2, nw * 32, X.dtype
+    if rows % 2:
+        raise BpdqError("planes: expected an even number of rows, those of the gate and as many of the other projection")
+    if group <= 0 or coefs_h.shape != (bits + 1, rows, d_in // group):
+        raise BpdqError("coefs_h: expected (bits + 1) x (2 d_out) x (d_in / group)")
+    if X.dim() != 2 or (dtype is not torch.bfloat16 and dtype is not torch.float16):
+        raise BpdqError("X: expected a float16 or bfloat16 matrix")
+    code = ACTS.get(act)
+    if code is None:
+        raise BpdqError(f"act: expected one of {sorted(ACTS)}")
+    n_tok = X.shape[0]
+    ldx = _rows(X, dtype, (n_tok, d_in), "X")
+    if Y is None:
+        Y = torch.empty((n_tok, d_out), dtype=dtype, device=X.device)
+        ldy = d_out
+    else:
+        ldy = _rows(Y, dtype, (n_tok, d_out), "Y")
+    if bias is not None and (bias.dtype is not dtype or bias.shape != (rows,) or not bias.is_cuda or not bias.is_contiguous()):
+        raise BpdqError(f"bias: expected a contiguous {dtype} vector of 2 d_out values on the GPU")
+    if ws is None:
+        ws = _scratch(lib.bpdq_linear_workspace_bytes(n_tok, d_in), X.device)
+    _here(X, planes, coefs_h, bias, Y, ws)
+    _call("bpdq_gated_linear", lib.bpdq_gated_linear(
+        planes.data_ptr(), coefs_h.data_ptr(), d_out, d_in, bits, group, X.data_ptr(), n_tok, ldx, DTYPES[dtype],
+        None if bias is None else bias.data_ptr(), code, Y.data_ptr(), ldy, *_ws(ws), _stream()))
+    return Y
+
+
+def _norm(X, weight, residual, S):
+    """The arguments that both norms begin with, and S."""
+    dtype = X.dtype
+    if X.dim() != 2 or dtype not in DTYPES:
+        raise BpdqError("X: expected a float32, float16 or bfloat16 matrix")
+    shape = n_tok, d = X.shape
+    ldx, ldr, lds, wide = _rows(X, dtype, shape, "X"), 0, 0, dtype
+    if weight is not None and (weight.dtype is not dtype or weight.shape != (d,) or not weight.is_cuda or not weight.is_contiguous()):
+        raise BpdqError(f"weight: expected a contiguous {dtype} vector of d values on the GPU")
+    if residual is not None:
+        wide = residual.dtype
+        if wide is not dtype and wide is not torch.float32:
+            raise BpdqError(f"residual: expected {dtype} or float32")
+        ldr = _rows(residual, wide, shape, "residual")
+        if S is None:
+            S = torch.empty(shape, dtype=wide, device=X.device)
+            lds = d
+        else:
+            lds = _rows(S, wide, shape, "S")
+    elif S is not None:
+        raise BpdqError("S: the sum, only with a residual")
+    return (X.data_ptr(), n_tok, d, ldx, DTYPES[dtype], None if residual is None else residual.data_ptr(), ldr, DTYPES[wide],
+            None if S is None else S.data_ptr(), lds, None if weight is None else weight.data_ptr()), S
+
+
+def bpdq_rms_norm(X, weight=None, eps=1e-6, residual=None, S=None, offset=0.0, Y=None):
+    """Returns (Y, S): S = X + residual (None without a residual), in the residual's type (X's or float32), and
+    Y = S / sqrt(mean(S^2) + eps) * (offset + weight) in X's.  S may be the residual, Y may be X."""
+    args, S = _norm(X, weight, residual, S)
+    if Y is None:
+        Y = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        ldy = X.shape[1]
+    else:
+        ldy = _rows(Y, X.dtype, X.shape, "Y")
+    _here(X, weight, residual, S, Y)
+    _call("bpdq_rms_norm", (_lib or load()).bpdq_rms_norm(*args, offset, eps, Y.data_ptr(), ldy, _stream()))
+    return Y, S
+
+
+def bpdq_rms_norm_q8(X, weight=None, eps=1e-6, residual=None, S=None, offset=0.0, group=0, codes=None, scales=None):
+    """bpdq_rms_norm with Y in 8 bits: returns (codes, scales, S), codes int8, scales float32 of n_tok x (d / group), one a row for group 0."""
+    args, S = _norm(X, weight, residual, S)
+    n_tok, d = X.shape
+    if codes is None:
+        codes = torch.empty((n_tok, d), dtype=torch.int8, device=X.device)
+    ldc = _rows(codes, torch.int8, (n_tok, d), "codes")
+    shape = (n_tok, d // group if group > 0 else 1)
+    if scales is None:
+        scales = torch.empty(shape, dtype=torch.float32, device=X.device)
+    _dev(scales, torch.float32, "scales")
+    if scales.shape != shape:
+        raise BpdqError("scales: expected n_tok x (d / group)")
+    _here(X, weight, residual, S, codes, scales)
+    _call("bpdq_rms_norm_q8", (_lib or load()).bpdq_rms_norm_q8(*args, offset, eps, group, codes.data_ptr(), ldc, scales.data_ptr(),
+                                                                _stream()))
+    return codes, scales, S
+
+
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+def bpdq_rotary_frequencies(rot, base=10000.0, scaling="plain", factor=1.0, low=1.0, high=32.0, original=4096):
+    """Radians per position of the rot / 2 pairs of channels (a float64 tensor on the host), and the factor on cosine and sine that goes with
+    them.  scaling: plain, linear, ntk, yarn or bands (include/bpdq.h); factor, low, high and original are those of the scaling."""
+    code = ROTARY_SCALINGS.get(scaling)
+    if code is None:
+        raise BpdqError(f"scaling: expected one of {sorted(ROTARY_SCALINGS)}")
+    freq, mscale = torch.empty(max(rot // 2, 1), dtype=torch.float64), ctypes.c_double()
+    _call("bpdq_rotary_frequencies", (_lib or load()).bpdq_rotary_frequencies(
+        rot, base, code, factor, low, high, original, freq.data_ptr(), ctypes.addressof(mscale)))
+    return freq, mscale.value
+
+
+def bpdq_rotary(freq, pos, tok_start, Q, K=None, max_tok=None, layout="half", mscale=1.0, inverse=False, Q_out=None, K_out=None):
+    """Rotary positions on Q (n_tok, n_q, head_dim) and K (n_tok, n_kv, head_dim): row tok_start[b] + i is at position pos[b] + i.  freq: float64
+    on the GPU, rot / 2 frequencies (bpdq_rotary_frequencies); channels from rot on pass.  Returns (Q_out, K_out), new unless given; Q_out may
+    be Q and K_out may be K.  max_tok: at least the largest count of a sequence (all rows, if it is not given)."""
+    _dev(freq, torch.float64, "freq")
+    _dev(pos, torch.int32, "pos")
+    _dev(tok_start, torch.int32, "tok_start")
+    n_seq, dtype = pos.numel(), Q.dtype
+    if tok_start.numel() != n_seq + 1:
+        raise BpdqError("tok_start: expected n_seq + 1 starts")
+    code = ROTARY_LAYOUTS.get(layout)
+    if code is None:
+        raise BpdqError(f"layout: expected one of {sorted(ROTARY_LAYOUTS)}")
+    if Q.dim() != 3 or dtype not in DTYPES:
+        raise BpdqError("Q: expected a float32, float16 or bfloat16 tensor of n_tok x n_q x head_dim")
+    n_tok, n_q, dim = Q.shape
+    ldq, ldqo = _rows(Q, dtype, Q.shape, "Q"), n_q * dim
+    if Q_out is None:
+        Q_out = torch.empty(Q.shape, dtype=dtype, device=Q.device)
+    else:
+        ldqo = _rows(Q_out, dtype, Q.shape, "Q_out")
+    n_kv = ldk = ldko = 0
+    k = k_out = None
+    if K is not None:
+        if K.dim() != 3 or K.shape[0] != n_tok or K.shape[2] != dim:
+            raise BpdqError("K: expected n_tok x n_kv x head_dim")
+        n_kv = K.shape[1]
+        ldk, ldko = _rows(K, dtype, K.shape, "K"), n_kv * dim
+        if K_out is None:
+            K_out = torch.empty(K.shape, dtype=dtype, device=K.device)
+        else:
+            ldko = _rows(K_out, dtype, K.shape, "K_out")
+        k, k_out = K.data_ptr(), K_out.data_ptr()
+    elif K_out is not None:
+        raise BpdqError("K_out: only with K")
+    _here(Q, freq, pos, tok_start, Q_out, K, K_out)
+    _call("bpdq_rotary", (_lib or load()).bpdq_rotary(
+        freq.data_ptr(), 2 * freq.numel(), code, mscale, 1 if inverse else 0, pos.data_ptr(), tok_start.data_ptr(), n_seq, n_tok,
+        n_tok if max_tok is None else max_tok, Q.data_ptr(), ldq, n_q, k, ldk, n_kv, dim, DTYPES[dtype], Q_out.data_ptr(), ldqo, k_out,
+        ldko, _stream()))
+    return Q_out, K_out
+
+
+def bpdq_sample_workspace_bytes(n_tok, n_vocab):
+    return load().bpdq_sample_workspace_bytes(n_tok, n_vocab)
+
+
+def bpdq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, prob=None, want_prob=False, ws=None):
+    """The next token of each row of logits (float32, float16 or bfloat16, n_tok x n_vocab) from the random numbers u (float32, n_tok, in [0, 1)):
+    temperature, top_p, min_p float32 and top_k int32, n_tok values each, or None.  Returns token (int32), or (token, prob) where prob (float32)
+    is given or wanted."""
+    lib = _lib or load()
+    dtype = logits.dtype
+    if logits.dim() != 2 or dtype not in DTYPES:
+        raise BpdqError("logits: expected a float32, float16 or bfloat16 matrix")
+    n_tok, n_vocab = logits.shape
+    ldl = _rows(logits, dtype, logits.shape, "logits")
+    if token is None:
+        token = torch.empty(n_tok, dtype=torch.int32, device=logits.device)
+    if prob is None and want_prob:
+        prob = torch.empty(n_tok, dtype=torch.float32, device=logits.device)
+    vectors = []
+    for t, kind, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+                          (min_p, torch.float32, "min_p"), (u, torch.float32, "u"), (token, torch.int32, "token"),
+                          (prob, torch.float32, "prob")):
+        if t is None:
+            vectors.append(None)
+            continue
+        if t.dtype is not kind or t.shape != (n_tok,) or not t.is_cuda or not t.is_contiguous():
+            raise BpdqError(f"{name}: expected a contiguous {kind} vector of n_tok values on the GPU")
+        vectors.append(t.data_ptr())
+    if ws is None:
+        ws = _scratch(lib.bpdq_sample_workspace_bytes(n_tok, n_vocab), logits.device)
+    _here(logits, temperature, top_k, top_p, min_p, u, token, prob, ws)
+    _call("bpdq_sample", lib.bpdq_sample(logits.data_ptr(), n_tok, n_vocab, ldl, DTYPES[dtype], *vectors, *_ws(ws), _stream()))
+    return token if prob is None else (token, prob)
 
 
 class KvCache:

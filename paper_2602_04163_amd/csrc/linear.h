@@ -71,6 +71,12 @@ __device__ __forceinline__ uint32_t linear_most(u32x4_t v, uint32_t most) {
   return most;
 }
 // eight consecutive values of X
+// GATED: the rows are those of two projections, gate and then up, of `half` rows each, and a tile takes them by eights in turn, so that
+// the eight of a gate and the eight of its up meet in one wavefront's epilogue.  The stored row of a tile's row v (past the end: the last):
+__device__ __forceinline__ int linear_pair_row(int v, int half) {
+  const int f = (v >> 4) * 8 + (v & 7);
+  return (f < half ? f : half - 1) + (v & 8 ? half : 0);
+}
 template <typename T>
 __device__ __forceinline__ u32x4_t linear_load8(const T* __restrict__ x, bool vec) {
   if (vec) return *reinterpret_cast<const u32x4_t*>(x);
@@ -126,7 +132,7 @@ constexpr int kRowPitch = 512 + 16;                       // bytes of a token's 
 // (Registers for one work-group to a CU: with the 128 of two, 16 rows spill, and 20 fp16 tokens of 11264 columns at 4 bits take 33 us, not 17.
 // With all 256 the forms of one row tile have none in scratch; of the others 14 do, 6 to 74 registers: twice 16 tokens with five row tiles but for
 // fp16 at one plane, with three at three and four planes, with two in bf16 at four, and eight row tiles at four.)
-template <typename T, int K, int R, int NT>
+template <typename T, int K, int R, int NT, bool GATED>
 __global__ __launch_bounds__(kLinThreads, 2) void linear_rows_kernel(LinearArgs a) {
   constexpr int kRows = 16 * R, kToks = 16 * NT;
   constexpr int kStageBytes = kLinWaves * 16 * kRowPitch, kPartBytes = kLinWaves * kToks * kRows * 4;
@@ -150,7 +156,8 @@ __global__ __launch_bounds__(kLinThreads, 2) void linear_rows_kernel(LinearArgs 
   u32x2_t w_next[K];
   _Float16 c_next[K + 1], c_next2[K + 1];                // of the first word and, where groups have an odd number of words, the second
   const bool odd = wpg % 2 != 0;
-  auto row = [&](int r) { return row0 + 16 * r + low < a.d_out ? row0 + 16 * r + low : a.d_out - 1; };
+  auto row = [&](int r) { return GATED ? linear_pair_row(row0 + 16 * r + low, a.d_out / 2)
+                                       : row0 + 16 * r + low < a.d_out ? row0 + 16 * r + low : a.d_out - 1; };
   auto load_c = [&](int r, int word, _Float16 (&c)[K + 1]) {
     const _Float16* p = a.coefs + (long)row(r) * n_grp + (word < nw ? word : 0) / wpg;
 #pragma unroll
@@ -277,6 +284,30 @@ __global__ __launch_bounds__(kLinThreads, 2) void linear_rows_kernel(LinearArgs 
     for (int n = 0; n < NT; ++n)
       *reinterpret_cast<f32x4_t*>(part + (wave * kToks + 16 * n + low) * kRows + 16 * r + 4 * quarter) = acc[r][n];
   __syncthreads();
+  if constexpr (GATED) {
+    const int f_all = a.d_out / 2;
+    for (int id = tid; id < kRows / 2 * kToks; id += kLinThreads) {
+      const int at = id % (kRows / 2), f = row0 / 2 + at, n = id / (kRows / 2), t = tok0 + n;
+      if (f >= f_all || t >= a.n_tok) continue;
+      const float* sum = part + n * kRows + 16 * (at / 8) + at % 8;
+      float gate = 0.f, up = 0.f;
+#pragma unroll
+      for (int s = 0; s < kLinWaves; ++s) {
+        gate += sum[s * kToks * kRows];
+        up += sum[s * kToks * kRows + 8];
+      }
+      if constexpr (kScale) {
+        gate *= linear_unscale(base_s[n]);
+        up *= linear_unscale(base_s[n]);
+      }
+      if (a.bias) {
+        gate += (float)static_cast<const T*>(a.bias)[f];
+        up += (float)static_cast<const T*>(a.bias)[f_all + f];
+      }
+      static_cast<T*>(a.y)[t * a.ldy + f] = (T)(linear_act(gate, a.act) * up);
+    }
+    return;
+  }
   for (int id = tid; id < kRows * kToks; id += kLinThreads) {
     const int r = row0 + id % kRows, t = tok0 + id / kRows;
     if (r >= a.d_out || t >= a.n_tok) continue;
@@ -412,6 +443,26 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
   }
 }
 
+// Eight values from `first` of one token of the gated product: both biases, activation, product, one rounding.
+template <typename T, int ACT>
+__device__ __forceinline__ void linear_finish_pairs(const LinearArgs& a, long tok, int first, const f32x4_t (&v)[4], float unscale,
+                                                    const float (&bias)[16]) {
+  typedef T T8 __attribute__((ext_vector_type(8)));
+  const int n = a.d_out / 2 - first < 8 ? a.d_out / 2 - first : 8;
+  T8 out;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    out[i] = (T)(linear_act<ACT>(v[i / 4][i % 4] * unscale + bias[i]) * (v[2 + i / 4][i % 4] * unscale + bias[8 + i]));
+  T* y = static_cast<T*>(a.y) + tok * a.ldy + first;
+  if (a.vec_y && n == 8) {
+    *reinterpret_cast<T8*>(y) = out;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) y[i] = out[i];
+  }
+}
+
 // Y tile of a work-group of wavefronts that share X.  What bounds it: the vector instructions that decode the weights, beside the matrix instructions, which share a SIMD's issue
 // (a stage takes about the longer of the two and 0.4 of the shorter), and the last round of tiles.  4096 bf16 tokens, 18944 x 3584 at 2 bits:
 // 517 to 612 us from card to card, some 50 of it GELU, 0.91 to 1.08 PFLOP/s (a library product of the dense 16-bit weights takes 500); 333 tokens,
@@ -427,7 +478,7 @@ __device__ __forceinline__ void linear_finish8(const LinearArgs& a, long tok, in
 // every wavefront has read the stage and the next one has landed.
 // The compiler does not see the LDS-DMA requests (inline assembly), so the vmcnt waits are written by hand: at most the requests of
 // the stages behind the next one may be outstanding.  Loads that the compiler issues meanwhile only make that wait longer.
-template <typename T, int K, typename S, int GS, bool VEC>
+template <typename T, int K, typename S, int GS, bool VEC, bool GATED>
 __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const uint32_t* __restrict__ base) {
   constexpr int W = kWords, RT = S::RT, TT = S::TT;
   extern __shared__ uint4 lds_raw[];
@@ -463,15 +514,18 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
 
   const char* w_base[K];
   const char* c_base[K + 1];
+  const int base_row = GATED ? 0 : row0;                 // (GATED: a plane is below 4 GB, and offsets are from its first row)
+  // the stored row of a tile's row, from base_row
+  auto stored = [&](int v) { return GATED ? linear_pair_row(row0 + v, a.d_out / 2) : row0 + v < a.d_out ? v : a.d_out - 1 - row0; };
 #pragma unroll
-  for (int i = 0; i < K; ++i) w_base[i] = reinterpret_cast<const char*>(a.planes + ((long)i * a.d_out + row0) * nw);
+  for (int i = 0; i < K; ++i) w_base[i] = reinterpret_cast<const char*>(a.planes + ((long)i * a.d_out + base_row) * nw);
 #pragma unroll
-  for (int i = 0; i <= K; ++i) c_base[i] = reinterpret_cast<const char*>(a.coefs + ((long)i * a.d_out + row0) * n_grp);
+  for (int i = 0; i <= K; ++i) c_base[i] = reinterpret_cast<const char*>(a.coefs + ((long)i * a.d_out + base_row) * n_grp);
   unsigned row[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     const int at = 32 * (RT * wr + r) + low;
-    row[r] = row0 + at < a.d_out ? at : a.d_out - 1 - row0;
+    row[r] = stored(at);
   }
   uint32_t w_cur[RT][K][W], w_next[RT][K][W];
   auto load_w = [&](int chunk) {                         // words past the end: the row's first, under levels of zero
@@ -513,7 +567,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int u = 0; u < kUnits; ++u) {
       const int id = u * S::kPart + tid, r = id % S::kRows, word = level_word(stage, id / S::kRows);
       const unsigned g = (unsigned)(word < nw ? word : 0) / (unsigned)wpg;
-      const unsigned at = row0 + r < a.d_out ? r : a.d_out - 1 - row0;
+      const unsigned at = stored(r);
 #pragma unroll
       for (int i = 0; i <= K; ++i)
         c_raw[u][i] = *reinterpret_cast<const _Float16*>(c_base[i] + (at * (unsigned)n_grp + g) * 2u);
@@ -662,11 +716,28 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   // lane holds rows 8 q + 4 half + i of token low.  (16-byte slot n of a token's 64 rows lies at n ^ (token & 15).)
   static_assert(RT == 2 && (size_t)S::WR * S::WT * 32 * 64 * 4 <= S::kLds, "16 slots a token");
   f32x4_t* mine = reinterpret_cast<f32x4_t*>(lds) + wave * 32 * 16;
-  const int s2 = 2 * (lane & 7), first = row0 + 64 * wr + 4 * s2;   // the lane's eight rows
-  float bias[8];
+  // (GATED: four lanes a token, a lane eight rows of each projection)
+  const int s2 = GATED ? 4 * (lane & 3) : 2 * (lane & 7), first = (row0 + 64 * wr + 4 * s2) / (GATED ? 2 : 1);   // the lane's eight rows
+  float bias[GATED ? 16 : 8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bias[i] = a.bias && first + i < a.d_out ? (float)static_cast<const T*>(a.bias)[first + i] : 0.f;
+  for (int i = 0; i < (GATED ? 16 : 8); ++i) {
+    const int at = GATED && i >= 8 ? a.d_out / 2 + first + i - 8 : first + i;
+    bias[i] = a.bias && first + i % 8 < (GATED ? a.d_out / 2 : a.d_out) ? (float)static_cast<const T*>(a.bias)[at] : 0.f;
+  }
   auto finish = [&](int t, auto act) {
+    if constexpr (GATED) {
+#pragma unroll 1
+      for (int it = 0; it < 2; ++it) {
+        const int k = it * 16 + (lane >> 2);
+        f32x4_t v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = mine[k * 16 + ((s2 + q) ^ (k & 15))];
+        const long tok = tok0 + 32 * (TT * wt + t) + k;
+        if (tok < a.n_tok && first < a.d_out / 2)
+          linear_finish_pairs<T, act.value>(a, tok, first, v, __is_same(T, _Float16) ? 1.f : linear_unscale(base[tok]), bias);
+      }
+      return;
+    } else {
 #pragma unroll 1
     for (int it = 0; it < 4; ++it) {
       const int k = it * 8 + (lane >> 3);
@@ -674,6 +745,7 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       const long tok = tok0 + 32 * (TT * wt + t) + k;
       if (tok < a.n_tok && first < a.d_out)
         linear_finish8<T, act.value>(a, tok, first, v0, v1, __is_same(T, _Float16) ? 1.f : linear_unscale(base[tok]), bias, a.vec_y, a.vec_r);
+    }
     }
   };
 #pragma unroll 1
@@ -700,15 +772,19 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   }
 }
 
-template <typename T, int K, typename S, int GS, bool VEC>
+// rows of the tiles of a call
+template <bool GATED>
+static int linear_tile_rows(int d_out) { return GATED ? bpdq_ceil_div(d_out / 2, 8) * 16 : d_out; }
+
+template <typename T, int K, typename S, int GS, bool VEC, bool GATED>
 static int linear_launch_as(const LinearArgs& a, dim3 grid, int tok_tiles, const uint32_t* base, hipStream_t stream) {
-  BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, GS, VEC>>(S::kLds)));
-  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, GS, VEC>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles, base);
+  BPDQ_HIP_TRY((bpdq_lds_limit<&linear_tiles_kernel<T, K, S, GS, VEC, GATED>>(S::kLds)));
+  hipLaunchKernelGGL((linear_tiles_kernel<T, K, S, GS, VEC, GATED>), grid, dim3(S::kThreads), S::kLds, stream, a, tok_tiles, base);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
 
-template <typename T, int K, typename S>
+template <typename T, int K, typename S, bool GATED>
 static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
   const int images = bpdq_ceil_div(a.d_in, 256) * 4 + (S::KS > 1), blocks = bpdq_ceil_div(a.n_tok, S::kToks) * (S::kToks / 32);
   // behind the images
@@ -720,58 +796,62 @@ static int linear_launch_tiles(const LinearArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL((linear_order_kernel<T>), dim3(bpdq_ceil_div(images * blocks, 4)), dim3(256), 0, stream, a, images * blocks, images, base);
   BPDQ_LAUNCH_CHECK();
   const int tok_tiles = bpdq_ceil_div(a.n_tok, S::kToks);
-  const dim3 grid(bpdq_ceil_div(a.d_out, S::kRows) * tok_tiles);
+  const dim3 grid(bpdq_ceil_div(linear_tile_rows<GATED>(a.d_out), S::kRows) * tok_tiles);
   const int wpg = a.group / 32;
   if (a.vec_w) {
-    if (wpg % 4 == 0) return linear_launch_as<T, K, S, 4, true>(a, grid, tok_tiles, base, stream);
-    if (wpg % 2 == 0) return linear_launch_as<T, K, S, 2, true>(a, grid, tok_tiles, base, stream);
-    return linear_launch_as<T, K, S, 1, true>(a, grid, tok_tiles, base, stream);
+    if (wpg % 4 == 0) return linear_launch_as<T, K, S, 4, true, GATED>(a, grid, tok_tiles, base, stream);
+    if (wpg % 2 == 0) return linear_launch_as<T, K, S, 2, true, GATED>(a, grid, tok_tiles, base, stream);
+    return linear_launch_as<T, K, S, 1, true, GATED>(a, grid, tok_tiles, base, stream);
   }
-  return linear_launch_as<T, K, S, 1, false>(a, grid, tok_tiles, base, stream);
+  return linear_launch_as<T, K, S, 1, false, GATED>(a, grid, tok_tiles, base, stream);
 }
 
-template <typename T, int K, int R, int NT>
+template <typename T, int K, int R, int NT, bool GATED>
 static int linear_launch(const LinearArgs& a, hipStream_t stream) {
-  const dim3 grid(bpdq_ceil_div(a.d_out, 16 * R), bpdq_ceil_div(a.n_tok, 16 * NT));
-  hipLaunchKernelGGL((linear_rows_kernel<T, K, R, NT>), grid, dim3(kLinThreads), 0, stream, a);
+  const dim3 grid(bpdq_ceil_div(linear_tile_rows<GATED>(a.d_out), 16 * R), bpdq_ceil_div(a.n_tok, 16 * NT));
+  hipLaunchKernelGGL((linear_rows_kernel<T, K, R, NT, GATED>), grid, dim3(kLinThreads), 0, stream, a);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
 
-template <typename T, int K, int NT>
+template <typename T, int K, int NT, bool GATED>
 static int linear_launch_rows(const LinearArgs& a, int r, hipStream_t stream) {
-  if (r == 2) return linear_launch<T, K, 2, NT>(a, stream);
-  if (r == 3) return linear_launch<T, K, 3, NT>(a, stream);
-  if (r == 5) return linear_launch<T, K, 5, NT>(a, stream);
+  if (r == 2) return linear_launch<T, K, 2, NT, GATED>(a, stream);
+  if (r == 3) return linear_launch<T, K, 3, NT, GATED>(a, stream);
+  if (r == 5) return linear_launch<T, K, 5, NT, GATED>(a, stream);
   if constexpr (NT == 1) {
-    if (r == 8) return linear_launch<T, K, 8, NT>(a, stream);
-    return linear_launch<T, K, 1, NT>(a, stream);
+    if (r == 8) return linear_launch<T, K, 8, NT, GATED>(a, stream);
+    return linear_launch<T, K, 1, NT, GATED>(a, stream);
   }
   return BPDQ_ERR_LAUNCH;                                // not offered
 }
 
-template <typename T, int K>
+template <typename T, int K, bool GATED>
 static int linear_pick(const LinearArgs& a, hipStream_t stream) {
-  const LinearPlan p = linear_plan(a.n_tok, a.d_in, a.d_out);
+  const LinearPlan p = linear_plan(a.n_tok, a.d_in, linear_tile_rows<GATED>(a.d_out));
   switch (p.kernel) {
-    case kRows1: return linear_launch_rows<T, K, 1>(a, p.r, stream);
-    case kRows2: return linear_launch_rows<T, K, 2>(a, p.r, stream);
-    case kTile256: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 8, 3>>(a, stream);
-    case kTile256x128: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 4, 3>>(a, stream);
-    case kTile128: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 2, 2, 4, 3>>(a, stream);
-    default: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 4, 2, 2, 3>>(a, stream);
+    case kRows1: return linear_launch_rows<T, K, 1, GATED>(a, p.r, stream);
+    case kRows2: return linear_launch_rows<T, K, 2, GATED>(a, p.r, stream);
+    case kTile256: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 8, 3>, GATED>(a, stream);
+    case kTile256x128: return linear_launch_tiles<T, K, LinearTile<K, 4, 1, 1, 2, 4, 3>, GATED>(a, stream);
+    case kTile128: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 2, 2, 4, 3>, GATED>(a, stream);
+    default: return linear_launch_tiles<T, K, LinearTile<K, 2, 1, 4, 2, 2, 3>, GATED>(a, stream);
   }
 }
 
-template <int K>
+template <int K, bool GATED>
 int linear_run(const LinearArgs& a, int dtype, hipStream_t stream) {
-  return dtype == BPDQ_F16 ? linear_pick<_Float16, K>(a, stream) : linear_pick<__bf16, K>(a, stream);
+  return dtype == BPDQ_F16 ? linear_pick<_Float16, K, GATED>(a, stream) : linear_pick<__bf16, K, GATED>(a, stream);
 }
 
-// instantiated in linear_k1.hip to linear_k4.hip
-extern template int linear_run<1>(const LinearArgs&, int, hipStream_t);
-extern template int linear_run<2>(const LinearArgs&, int, hipStream_t);
-extern template int linear_run<3>(const LinearArgs&, int, hipStream_t);
-extern template int linear_run<4>(const LinearArgs&, int, hipStream_t);
+// instantiated in linear_k1.hip to linear_k4.hip, and gated_k1.hip to gated_k4.hip
+extern template int linear_run<1, false>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<2, false>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<3, false>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<4, false>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<1, true>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<2, true>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<3, true>(const LinearArgs&, int, hipStream_t);
+extern template int linear_run<4, true>(const LinearArgs&, int, hipStream_t);
 
 }  // namespace bpdq

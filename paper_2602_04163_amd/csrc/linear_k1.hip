@@ -2,5 +2,5 @@
 #include "linear.h"
 
 namespace bpdq {
-template int linear_run<1>(const LinearArgs&, int, hipStream_t);
+template int linear_run<1, false>(const LinearArgs&, int, hipStream_t);
 }

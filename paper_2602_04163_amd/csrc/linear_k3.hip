@@ -2,5 +2,5 @@
 #include "linear.h"
 
 namespace bpdq {
-template int linear_run<3>(const LinearArgs&, int, hipStream_t);
+template int linear_run<3, false>(const LinearArgs&, int, hipStream_t);
 }

@@ -1,0 +1,293 @@
+// Root-mean-square norm with the residual's addition:
+//   s = x + r,   y = s / sqrt(mean(s^2) + eps) * (offset + w),   and in 8 bits: scale = max(amax |y|, 2^-96) / 127, code = rint(y / scale).
+//
+// A row stays in registers from its one load to its stores: eight consecutive values to a thread and turn, so that every access is 16 bytes a
+// lane and whole lines a wavefront.  Squares are summed in fp64, where neither 3e38 nor 1e-30 leaves the range; from there on fp32, y from the
+// unrounded sum.
+//
+// What bounds it: bytes, and for few rows the launch.
+#include "common.h"
+
+namespace bpdq {
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kNormMost = 65536;                          // values of a row: 1024 threads of eight turns
+constexpr float kNormFloor = 0x1p-96f;                    // the least magnitude a scale is made for, as in the cache
+
+struct NormArgs {
+  const void* x;
+  const void* residual;
+  const void* weight;
+  void* sum;
+  void* y;
+  int8_t* codes;
+  float* scales;
+  long ldx, ldr, lds, ldy, ldc;
+  int n_tok, d, group;
+  float offset, eps;
+  int vec_x, vec_r, vec_s, vec_w, vec_y;                  // by 16 bytes (codes: by 8)
+};
+
+template <typename T>
+__device__ __forceinline__ void norm_load8(const T* __restrict__ p, bool vec, int n, float (&v)[8]) {
+  if (vec && n >= 8) {
+    alignas(16) T raw[8];
+#pragma unroll
+    for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(raw)[q] = reinterpret_cast<const u32x4_t*>(p)[q];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)p[e] : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void norm_store8(T* __restrict__ p, bool vec, int n, const float (&v)[8]) {
+  if (vec && n >= 8) {
+    alignas(16) T raw[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) raw[e] = (T)v[e];
+#pragma unroll
+    for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(p)[q] = reinterpret_cast<const u32x4_t*>(raw)[q];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = (T)v[e];
+  }
+}
+
+// T: X, weight, Y; R: residual and sum; NV: turns of a thread.  blockDim.x = threads of a row, blockDim.y rows (1 unless a row is one wavefront's).
+template <typename T, typename R, int NV, bool Q8>
+__global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
+  const int tid = threadIdx.x, per = blockDim.x, waves = per >> 6;
+  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  __shared__ double part_sum[16];
+  __shared__ uint32_t part_most[16];
+  if (row >= a.n_tok) return;                             // whole wavefronts, and only where rows are wavefronts' own
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  const R* r = a.residual ? static_cast<const R*>(a.residual) + row * a.ldr : nullptr;
+  float v[NV][8], w[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = 8 * (j * per + tid);
+    norm_load8(x + at, a.vec_x, a.d - at, v[j]);
+  }
+  if (r) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = 8 * (j * per + tid);
+      float add[8];
+      norm_load8(r + at, a.vec_r, a.d - at, add);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] += add[e];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int at = 8 * (j * per + tid);
+    if (a.weight) norm_load8(static_cast<const T*>(a.weight) + at, a.vec_w, a.d - at, w[j]);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[j][e] = 1.f;
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fma((double)v[j][e], (double)v[j][e], sum);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (waves > 1) {
+    if ((tid & 63) == 0) part_sum[tid >> 6] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int q = 0; q < waves; ++q) sum += part_sum[q];
+  }
+  const float inv_rms = (float)rsqrt(sum / a.d + (double)a.eps);
+  if (a.sum) {
+    R* s = static_cast<R*>(a.sum) + row * a.lds;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = 8 * (j * per + tid);
+      norm_store8(s + at, a.vec_s, a.d - at, v[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[j][e] *= inv_rms * (a.offset + w[j][e]);
+  if constexpr (!Q8) {
+    T* y = static_cast<T*>(a.y) + row * a.ldy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = 8 * (j * per + tid);
+      norm_store8(y + at, a.vec_y, a.d - at, v[j]);
+    }
+  } else {
+    // largest magnitudes as bits: a NaN is above an infinity, an infinity above every number
+    uint32_t most[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      most[j] = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = 8 * (j * per + tid) + e < a.d ? __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu : 0u;
+        most[j] = most[j] > b ? most[j] : b;
+      }
+    }
+    if (a.group == 0) {
+#pragma unroll
+      for (int j = 1; j < NV; ++j) most[0] = most[0] > most[j] ? most[0] : most[j];
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const uint32_t b = __shfl_xor(most[0], o, 64);
+        most[0] = most[0] > b ? most[0] : b;
+      }
+      if (waves > 1) {
+        if ((tid & 63) == 0) part_most[tid >> 6] = most[0];
+        __syncthreads();
+        for (int q = 0; q < waves; ++q) most[0] = most[0] > part_most[q] ? most[0] : part_most[q];
+      }
+#pragma unroll
+      for (int j = 1; j < NV; ++j) most[j] = most[0];
+    } else {
+      for (int o = a.group / 16; o > 0; o >>= 1) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const uint32_t b = __shfl_xor(most[j], o, 64);
+          most[j] = most[j] > b ? most[j] : b;
+        }
+      }
+    }
+    const int n_scale = a.group ? a.d / a.group : 1;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int at = 8 * (j * per + tid);
+      if (at >= a.d) break;
+      const float scale = most[j] >= 0x7f800000u ? __builtin_nanf("")
+                                                 : fmaxf(__builtin_bit_cast(float, most[j]), kNormFloor) * (1.0f / 127.0f);
+      const int unit = a.group ? a.group : a.d;
+      if (at % unit == 0) a.scales[(long)row * n_scale + at / unit] = scale;
+      const float inv = 1.f / scale;
+      int8_t* c = a.codes + row * a.ldc + at;
+      uint32_t out[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e)                         // (a NaN becomes the lower bound)
+        out[e / 4] |= (uint32_t)((int)fminf(fmaxf(rintf(v[j][e] * inv), -127.f), 127.f) & 255) << (8 * (e % 4));
+      if (a.vec_y && a.d - at >= 8) {
+        *reinterpret_cast<u32x2_t*>(c) = u32x2_t{out[0], out[1]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at + e < a.d) c[e] = (int8_t)(out[e / 4] >> (8 * (e % 4)));
+      }
+    }
+  }
+}
+
+template <typename T, typename R, int NV, bool Q8>
+static int norm_launch(const NormArgs& a, hipStream_t stream) {
+  const int turns = bpdq_ceil_div(bpdq_ceil_div(a.d, 8), NV);
+  const int per = bpdq_ceil_div(turns, 64) * 64, rows = per == 64 ? 4 : 1;
+  hipLaunchKernelGGL((norm_kernel<T, R, NV, Q8>), dim3(bpdq_ceil_div(a.n_tok, rows)), dim3(per, rows), 0, stream, a);
+  BPDQ_LAUNCH_CHECK();
+  return 0;
+}
+
+template <typename T, typename R, bool Q8>
+static int norm_pick(const NormArgs& a, hipStream_t stream) {
+  const int vecs = bpdq_ceil_div(a.d, 8);
+  if (vecs <= 1024) return norm_launch<T, R, 1, Q8>(a, stream);
+  if (vecs <= 2048) return norm_launch<T, R, 2, Q8>(a, stream);
+  if (vecs <= 4096) return norm_launch<T, R, 4, Q8>(a, stream);
+  return norm_launch<T, R, 8, Q8>(a, stream);
+}
+
+template <bool Q8>
+static int norm_by_type(const NormArgs& a, int dtype, int rdtype, hipStream_t stream) {
+  if (dtype == BPDQ_F32) return norm_pick<float, float, Q8>(a, stream);
+  if (dtype == BPDQ_F16)
+    return rdtype == BPDQ_F16 ? norm_pick<_Float16, _Float16, Q8>(a, stream) : norm_pick<_Float16, float, Q8>(a, stream);
+  return rdtype == BPDQ_BF16 ? norm_pick<__bf16, __bf16, Q8>(a, stream) : norm_pick<__bf16, float, Q8>(a, stream);
+}
+
+static bool norm_vec(const void* p, long ld, size_t size, size_t unit = 16) {
+  return reinterpret_cast<uintptr_t>(p) % unit == 0 && (size_t)ld * size % unit == 0;
+}
+static bool norm_type(int dtype) { return dtype == BPDQ_F32 || dtype == BPDQ_F16 || dtype == BPDQ_BF16; }
+
+// what both entries check and fill in; a negative code, or 0, or 1 where there is nothing to do
+static int norm_args(NormArgs& a, const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype,
+                     void* S, long lds, const void* weight, float offset, float eps) {
+  if (n_tok < 0) return -2;
+  if (d <= 0 || d > kNormMost) return -3;
+  if (!norm_type(dtype)) return -5;
+  if (residual && rdtype != dtype && rdtype != BPDQ_F32) return -8;
+  if (!(offset - offset == 0.f)) return -12;
+  if (!(eps >= 0x1p-126f) || !(eps - eps == 0.f)) return -13;
+  if (n_tok == 0) return 1;
+  const size_t size = dtype == BPDQ_F32 ? 4 : 2, wide = residual && rdtype == BPDQ_F32 ? 4 : size;
+  if (!X || reinterpret_cast<uintptr_t>(X) % size) return -1;
+  if (ldx < d) return -4;
+  if (reinterpret_cast<uintptr_t>(residual) % wide) return -6;
+  if (residual && ldr < d) return -7;
+  if (S && (!residual || reinterpret_cast<uintptr_t>(S) % wide)) return -9;
+  if (S && lds < d) return -10;
+  if (reinterpret_cast<uintptr_t>(weight) % size) return -11;
+  a = NormArgs{};
+  a.x = X;
+  a.residual = residual;
+  a.weight = weight;
+  a.sum = S;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.lds = lds;
+  a.n_tok = n_tok;
+  a.d = d;
+  a.offset = offset;
+  a.eps = eps;
+  a.vec_x = norm_vec(X, ldx, size);
+  a.vec_r = norm_vec(residual, ldr, wide);
+  a.vec_s = norm_vec(S, lds, wide);
+  a.vec_w = norm_vec(weight, 0, size);
+  return 0;
+}
+
+}  // namespace bpdq
+
+using namespace bpdq;
+
+extern "C" int bpdq_rms_norm(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype,
+                             void* S, long lds, const void* weight, float offset, float eps, void* Y, long ldy, void* stream) {
+  NormArgs a;
+  const int rc = norm_args(a, X, n_tok, d, ldx, dtype, residual, ldr, rdtype, S, lds, weight, offset, eps);
+  if (rc) return rc < 0 ? rc : 0;
+  const size_t size = dtype == BPDQ_F32 ? 4 : 2;
+  if (!Y || reinterpret_cast<uintptr_t>(Y) % size) return -14;
+  if (ldy < d) return -15;
+  a.y = Y;
+  a.ldy = ldy;
+  a.vec_y = norm_vec(Y, ldy, size);
+  return norm_by_type<false>(a, dtype, residual ? rdtype : dtype, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int bpdq_rms_norm_q8(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype,
+                                void* S, long lds, const void* weight, float offset, float eps, int group, int8_t* codes, long ldc,
+                                float* scales, void* stream) {
+  NormArgs a;
+  const int rc = norm_args(a, X, n_tok, d, ldx, dtype, residual, ldr, rdtype, S, lds, weight, offset, eps);
+  if (rc < 0) return rc;
+  if (group != 0 && ((group != 32 && group != 64 && group != 128 && group != 256) || d % group)) return -14;
+  if (rc) return 0;
+  if (!codes) return -15;
+  if (ldc < d) return -16;
+  if (!scales || (reinterpret_cast<uintptr_t>(scales) & 3)) return -17;
+  a.codes = codes;
+  a.scales = scales;
+  a.ldc = ldc;
+  a.group = group;
+  a.vec_y = norm_vec(codes, ldc, 1, 8);
+  return norm_by_type<true>(a, dtype, residual ? rdtype : dtype, static_cast<hipStream_t>(stream));
+}
