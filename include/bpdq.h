@@ -343,7 +343,7 @@ int bpdq_rotary_frequencies(int rot, double base, int scaling, double factor, do
  * A value of minus infinity or NaN is not there; a row where nothing is there gets token -1 and prob 0.  Plus infinities share the row equally.
  * Weights are counted in units of 2^-43 of the largest (a token below half a unit is never drawn and adds nothing), their sums are exact, and the
  * result is the same from run to run.
- * Requirements: n_vocab <= 2^20; ws 256-byte aligned, of bpdq_sample_workspace_bytes() bytes; any alignment of the elements.  n_tok = 0 launches nothing.
+ * Requirements: n_tok <= 32768, n_vocab <= 2^20; ws 256-byte aligned, of bpdq_sample_workspace_bytes() bytes; any alignment of the elements.  n_tok = 0 launches nothing.
  * Returns 0, or a negative code naming the argument (-1 logits, -2 n_tok, -3 n_vocab, -4 ldl, -5 dtype, -6 temperature, -7 top_k, -8 top_p,
  * -9 min_p, -10 u, -11 token, -12 prob, -13 ws, -14 ws_bytes). */
 size_t bpdq_sample_workspace_bytes(int n_tok, int n_vocab);

@@ -112,7 +112,7 @@ SAMPLE = dict(logits=P, n_tok=3, n_vocab=1000, ldl=1000, dtype=2, temperature=P,
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(logits=None), -1), (dict(logits=P + 1), -1), (dict(logits=P + 2, dtype=0), -1), (dict(n_tok=-1), -2), (dict(n_vocab=0), -3),
+    (dict(logits=None), -1), (dict(logits=P + 1), -1), (dict(logits=P + 2, dtype=0), -1), (dict(n_tok=-1), -2), (dict(n_tok=(1 << 15) + 1), -2), (dict(n_vocab=0), -3),
     (dict(n_vocab=(1 << 20) + 1), -3), (dict(ldl=999), -4), (dict(dtype=3), -5), (dict(dtype=-1), -5), (dict(temperature=P + 2), -6),
     (dict(top_k=P + 1), -7), (dict(top_p=P + 2), -8), (dict(min_p=P + 3), -9), (dict(u=None), -10), (dict(u=P + 2), -10), (dict(token=None), -11),
     (dict(token=P + 1), -11), (dict(prob=P + 2), -12), (dict(n_tok=0, logits=None, u=None, token=None, ws=None, ws_bytes=0), 0)])
@@ -128,4 +128,4 @@ def test_sample_wants_its_workspace(lib):
         assert lib.bpdq_sample(*{**SAMPLE, "ws": None}.values()) == -13
         assert lib.bpdq_sample(*{**SAMPLE, "ws": P + 64}.values()) == -13
         assert lib.bpdq_sample(*{**SAMPLE, "ws_bytes": need - 1}.values()) == -14
-    assert size(1 << 20, 1 << 20) >= size(1 << 10, 1 << 20)
+    assert size(1 << 15, 1 << 20) > size(1 << 10, 1 << 20) > 0 and size((1 << 15) + 1, 1000) == 0
