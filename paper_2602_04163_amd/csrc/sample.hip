@@ -12,6 +12,9 @@
 
 namespace bpdq {
 
+typedef unsigned long long u64_t;
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleVocabMost = 1 << 20;                 // 2^20 weights of at most 2^43 fit into 63 bits
 constexpr int kSampleRowsMost = 1 << 15;                  // times 256 chunks of 256 threads: within the grid's 2^32
@@ -28,7 +31,7 @@ struct SampleArgs {
   int* token;
   float* prob;
   long ld;
-  int n_tok, n_vocab, vec;
+  int n_tok, n_vocab;
 };
 
 // Larger values have larger keys; 0: not there (minus infinity, or no number).
@@ -37,6 +40,10 @@ __device__ __forceinline__ uint32_t sample_key(float x) {
   const uint32_t k = b >> 31 ? ~b : b | 0x80000000u;
   return x > -__builtin_inff() ? k : 0u;
 }
+// key and index as one number: larger values first, of equal ones the lower index
+__device__ __forceinline__ u64_t sample_place(uint32_t key, int i) { return (u64_t)key << 20 | (u64_t)(kSampleVocabMost - 1 - i); }
+__device__ __forceinline__ int sample_index(u64_t place) { return kSampleVocabMost - 1 - (int)(place & (kSampleVocabMost - 1)); }
+__device__ __forceinline__ uint32_t sample_key_of(u64_t place) { return (uint32_t)(place >> 20); }
 __device__ __forceinline__ float sample_value(uint32_t key) {
   return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key);
 }
@@ -74,67 +81,100 @@ __device__ __forceinline__ unsigned long long sample_share(float part, unsigned 
   return (unsigned long long)whole + (up && (whole << shift) != full);
 }
 
-typedef unsigned long long u64_t;
+// Inclusive sums (MAX: maxima) over the lanes up to each one, by DPP: within rows of 16, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64_t sample_dpp(u64_t v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (u64_t)hi << 32 | lo;                            // (lanes without a source: 0)
+}
+template <bool MAX>
+__device__ __forceinline__ u64_t sample_wave_scan(u64_t v) {
+  auto join = [](u64_t a, u64_t b) { return MAX ? (a > b ? a : b) : a + b; };
+  v = join(v, sample_dpp<0x111, 0xf>(v));                 // row_shr 1, 2, 4, 8
+  v = join(v, sample_dpp<0x112, 0xf>(v));
+  v = join(v, sample_dpp<0x114, 0xf>(v));
+  v = join(v, sample_dpp<0x118, 0xf>(v));
+  v = join(v, sample_dpp<0x142, 0xa>(v));                 // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+  v = join(v, sample_dpp<0x143, 0xc>(v));
+  return v;
+}
+__device__ __forceinline__ u64_t sample_lane(u64_t v, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
+  return (u64_t)hi << 32 | lo;
+}
 
-struct SampleShared {
-  u64_t hist[kSampleBins];
-  u64_t part[kSampleThreads / 64 + 2];
-  u64_t before, value;
-  int bin;
+// Sums and maxima over a work-group, and over the threads up to each one: one barrier each.  (Partial results lie in two places in turn: who
+// writes the first again has passed the barrier of the second, which all reach behind their reading of the first.)
+template <int kThreads>
+struct SampleGroup {
+  static constexpr int kWaves = kThreads / 64;
+  u64_t (&part)[2][kWaves];
+  int turn = 0;
+  __device__ __forceinline__ explicit SampleGroup(u64_t (&p)[2][kWaves]) : part(p) {}
+
+  template <bool MAX>
+  __device__ __forceinline__ u64_t all(u64_t v) {
+    v = sample_wave_scan<MAX>(v);
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) part[turn][threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v = MAX ? (v > part[turn][w] ? v : part[turn][w]) : v + part[turn][w];
+    return v;
+  }
+  __device__ __forceinline__ u64_t sum(u64_t v) { return all<false>(v); }
+  __device__ __forceinline__ u64_t max(u64_t v) { return all<true>(v); }
+  __device__ __forceinline__ u64_t scan(u64_t v, u64_t& total) {
+    v = sample_wave_scan<false>(v);
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 63) part[turn][threadIdx.x >> 6] = v;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w == (int)(threadIdx.x >> 6)) v += total;
+      total += part[turn][w];
+    }
+    return v;
+  }
 };
 
-__device__ __forceinline__ u64_t sample_sum(SampleShared& sh, u64_t v) {
-  const int tid = threadIdx.x;
+// the running sum at which the token is
+__device__ __forceinline__ u64_t sample_draw(float u, u64_t total) {
+  const u64_t target = u > 0.f ? sample_share(u < 1.f ? u : 1.f, total, false) + 1 : 1;
+  return target < total ? target : total;
+}
+
+// A row's values by their place j = index + skew in 16-byte blocks: block j / 8 can be loaded whole, whatever the row's address.
+template <typename T>
+__device__ __forceinline__ int sample_skew(const T* x) { return (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) % (16 / sizeof(T))); }
+
+// values at .. at + 7 of a row, minus infinity where it has none
+template <typename T>
+struct SampleEight {
+  alignas(16) T raw[8];
+  __device__ __forceinline__ void load(const T* __restrict__ x, int at, int n_vocab) {
+    if (at >= 0 && at + 8 <= n_vocab) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((tid & 63) == 0) sh.part[tid >> 6] = v;
-  __syncthreads();
-  v = 0;
-  for (int w = 0; w < kSampleThreads / 64; ++w) v += sh.part[w];
-  return v;
-}
-__device__ __forceinline__ u64_t sample_max(SampleShared& sh, u64_t v) {
-  const int tid = threadIdx.x;
+      for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(raw)[q] = reinterpret_cast<const u32x4_t*>(x + at)[q];
+    } else {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const u64_t b = __shfl_xor(v, o, 64);
-    v = v > b ? v : b;
+      for (int e = 0; e < 8; ++e) raw[e] = at + e >= 0 && at + e < n_vocab ? x[at + e] : (T)(-__builtin_inff());
+    }
   }
-  __syncthreads();
-  if ((tid & 63) == 0) sh.part[tid >> 6] = v;
-  __syncthreads();
-  for (int w = 0; w < kSampleThreads / 64; ++w) v = v > sh.part[w] ? v : sh.part[w];
-  return v;
-}
-__device__ __forceinline__ void sample_clear(SampleShared& sh) {
-  __syncthreads();
-  sh.hist[threadIdx.x] = 0;
-  __syncthreads();
-}
-// The first of `bins` bins, from the top if `down`, where the running sum reaches `target` (>= 1): sh.bin (-1: none), sh.before and sh.value.
-__device__ __forceinline__ void sample_find(SampleShared& sh, int bins, bool down, u64_t target) {
-  const int tid = threadIdx.x;
-  __syncthreads();
-  const int bin = down ? bins - 1 - tid : tid;
-  const u64_t mine = tid < bins ? sh.hist[bin] : 0;
-  u64_t v = mine;
+  // f(value, index) of what is there
+  template <typename F>
+  __device__ __forceinline__ void each(int at, F f) const {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64_t b = __shfl_up(v, o, 64);
-    if ((tid & 63) >= o) v += b;
+    for (int e = 0; e < 8; ++e) {
+      const float v = (float)raw[e] + 0.f;                // (minus zero is zero)
+      if (v > -__builtin_inff()) f(v, at + e);
+    }
   }
-  if ((tid & 63) == 63) sh.part[tid >> 6] = v;
-  if (tid == 0) sh.bin = -1;
-  __syncthreads();
-  for (int w = 0; w < (tid >> 6); ++w) v += sh.part[w];
-  if (v >= target && v - mine < target) {
-    sh.bin = bin;
-    sh.before = v - mine;
-    sh.value = mine;
-  }
-  __syncthreads();
-}
+};
 
 // ---------------------------------------------------------------- rows cut into chunks
 //
@@ -154,18 +194,27 @@ constexpr int kSampleChunks = 256;                        // of a row, at most
 constexpr int kSampleSteps = 3072;                        // 12 octaves of 256, from 2^-5 below the largest value to 2^7
 constexpr int kSampleList = 2048;
 
-__host__ __device__ static inline int sample_turns(int n_tok, int n_vocab) {       // of a chunk
+static int sample_chunks(int n_vocab, int turns) { return bpdq_ceil_div(n_vocab + 7, turns * kSampleTurn); }        // (with the skew)
+static int sample_turns(int n_tok, int n_vocab) {         // of a chunk
   int turns = 1;
-  while ((long)n_tok * bpdq_ceil_div(n_vocab, turns * kSampleTurn) > 2048 && turns < 8) ++turns;
-  while (bpdq_ceil_div(n_vocab, turns * kSampleTurn) > kSampleChunks) ++turns;
+  while ((long)n_tok * sample_chunks(n_vocab, turns) > 2048 && turns < 8) ++turns;
+  while (sample_chunks(n_vocab, turns) > kSampleChunks) ++turns;
   return turns;
 }
+
+// What is known of a row before its exact border.
+struct SampleBorder {
+  u64_t top;                                              // its largest value
+  u64_t target, before;                                   // counts or weights: what is to be reached, and what lies above the bin
+  u64_t bin;                                              // of the histogram; kSampleSteps: nothing is bounded
+};
 
 struct SampleWork {
   u64_t* top;                                             // [row][chunk]
   u64_t* sum;                                             // [row][chunk]
   u64_t* hist;                                            // [row][kSampleSteps]
   u64_t* list;                                            // [row][kSampleList]
+  SampleBorder* border;                                   // [row]
   int* count;                                             // [row] of the list; above kSampleList: it did not fit
   int chunks, turns;
 };
@@ -173,12 +222,13 @@ struct SampleWork {
 static size_t sample_work(SampleWork& w, void* ws, int n_tok, int n_vocab) {
   BpdqArena arena(ws);
   w.turns = sample_turns(n_tok, n_vocab);
-  w.chunks = bpdq_ceil_div(n_vocab, w.turns * kSampleTurn);
+  w.chunks = sample_chunks(n_vocab, w.turns);
   const size_t n = n_tok;
   w.top = arena.take<u64_t>(n * w.chunks);
   w.sum = arena.take<u64_t>(n * w.chunks);
   w.hist = arena.take<u64_t>(n * kSampleSteps);
   w.list = arena.take<u64_t>(n * kSampleList);
+  w.border = arena.take<SampleBorder>(n);
   w.count = arena.take<int>(n);
   return arena.off;
 }
@@ -196,7 +246,7 @@ __device__ __forceinline__ SampleAsk sample_ask(const SampleArgs& a, int row, u6
   SampleAsk ask;
   const float t = a.temperature ? a.temperature[row] : 1.f;
   ask.draw = top != 0 && t > 0.f;
-  ask.most = sample_value((uint32_t)(top >> 32));
+  ask.most = sample_value(sample_key_of(top));
   ask.per = 1.4426950408889634074 / (double)t;
   const int k = a.top_k ? a.top_k[row] : 0;
   ask.k = k > 0 && k < a.n_vocab ? k : 0;
@@ -214,77 +264,68 @@ __device__ __forceinline__ int sample_step(float x, float most) {
   return step < 0 ? 0 : step < kSampleSteps ? step : kSampleSteps - 1;
 }
 
-// f(value, index) of the chunk's values that are there
-template <typename T, typename F>
-__device__ __forceinline__ void sample_each(const SampleArgs& a, const T* __restrict__ x, int first, int end, bool vec, F f) {
-  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-  for (int at = first + 8 * threadIdx.x; at < end; at += 8 * blockDim.x) {
-    alignas(16) T raw[8];
-    if (vec && at + 8 <= end) {
-#pragma unroll
-      for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(raw)[q] = reinterpret_cast<const u32x4_t*>(x + at)[q];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) raw[e] = at + e < end ? x[at + e] : (T)(-__builtin_inff());
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float v = (float)raw[e] + 0.f;                // (minus zero is zero)
-      if (v > -__builtin_inff()) f(v, at + e);
+// A chunk's values, the first turn's loaded at once.
+template <typename T>
+struct SampleChunk {
+  const T* x;
+  int first, turns, n_vocab;
+  SampleEight<T> eight;
+  __device__ __forceinline__ SampleChunk(const SampleArgs& a, const SampleWork& w, int row, int chunk)
+      : x(static_cast<const T*>(a.logits) + row * a.ld), turns(w.turns), n_vocab(a.n_vocab) {
+    first = chunk * turns * kSampleTurn + 8 * (int)threadIdx.x - sample_skew(x);
+    eight.load(x, first, n_vocab);
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {
+    for (int turn = 0; turn < turns; ++turn) {
+      const int at = first + turn * kSampleTurn;
+      SampleEight<T> next;
+      if (turn + 1 < turns) next.load(x, at + kSampleTurn, n_vocab);
+      eight.each(at, f);
+      eight = next;
     }
   }
-}
+};
 
-template <typename V, typename F>
-__device__ __forceinline__ V sample_fold(V v, V* part, F f) {        // over a work-group of kSampleChunkThreads
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = f(v, (V)__shfl_xor(v, o, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = part[0];
-#pragma unroll
-  for (int w = 1; w < kSampleChunkThreads / 64; ++w) v = f(v, part[w]);
-  return v;
-}
-__device__ __forceinline__ u64_t sample_larger(u64_t a, u64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ u64_t sample_add(u64_t a, u64_t b) { return a + b; }
+typedef SampleGroup<kSampleChunkThreads> SampleChunkGroup;
 
 // the row's largest, from its chunks'
-__device__ __forceinline__ u64_t sample_row_top(const SampleWork& w, int row, u64_t* part) {
-  const u64_t mine = threadIdx.x < (unsigned)w.chunks ? w.top[(long)row * w.chunks + threadIdx.x] : 0;
-  return sample_fold(mine, part, sample_larger);
+__device__ __forceinline__ u64_t sample_row_top(const SampleWork& w, int row, SampleChunkGroup& group) {
+  return group.max(threadIdx.x < (unsigned)w.chunks ? w.top[(long)row * w.chunks + threadIdx.x] : 0);
 }
 
 template <typename T>
 __global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleArgs a, SampleWork w, bool clear) {
-  __shared__ u64_t part[kSampleChunkThreads / 64];
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, first = chunk * w.turns * kSampleTurn;
-  const int end = first + w.turns * kSampleTurn < a.n_vocab ? first + w.turns * kSampleTurn : a.n_vocab;
-  u64_t top = 0;
-  sample_each(a, static_cast<const T*>(a.logits) + row * a.ld, first, end, a.vec, [&](float v, int i) {
-    top = sample_larger(top, (u64_t)sample_key(v) << 32 | (uint32_t)~i);
-  });
-  top = sample_fold(top, part, sample_larger);
-  if (threadIdx.x == 0) w.top[blockIdx.x] = top;
+  __shared__ u64_t part[2][kSampleChunkThreads / 64];
+  SampleChunkGroup group(part);
+  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks;
+  SampleChunk<T> values(a, w, row, chunk);
   if (clear) {
     for (int i = chunk * kSampleChunkThreads + threadIdx.x; i < kSampleSteps; i += w.chunks * kSampleChunkThreads)
       w.hist[(long)row * kSampleSteps + i] = 0;
     if (chunk == 0 && threadIdx.x == 0) w.count[row] = 0;
   }
+  u64_t top = 0;
+  values.each([&](float v, int i) {
+    const u64_t place = sample_place(sample_key(v), i);
+    top = top > place ? top : place;
+  });
+  top = group.max(top);
+  if (threadIdx.x == 0) w.top[blockIdx.x] = top;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(SampleArgs a, SampleWork w) {
   __shared__ u64_t hist[kSampleSteps];
-  __shared__ u64_t part[kSampleChunkThreads / 64];
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, first = chunk * w.turns * kSampleTurn;
-  const int end = first + w.turns * kSampleTurn < a.n_vocab ? first + w.turns * kSampleTurn : a.n_vocab;
-  const SampleAsk ask = sample_ask(a, row, sample_row_top(w, row, part));
-  if (!ask.draw || (ask.k == 0 && ask.p == 1.f)) return; // uniform
+  __shared__ u64_t part[2][kSampleChunkThreads / 64];
+  SampleChunkGroup group(part);
+  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks;
+  if (!(a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.n_vocab) && !(a.top_p && a.top_p[row] < 1.f)) return;   // uniform: nothing to bound
+  SampleChunk<T> values(a, w, row, chunk);
   for (int i = threadIdx.x; i < kSampleSteps; i += kSampleChunkThreads) hist[i] = 0;
-  __syncthreads();
-  sample_each(a, static_cast<const T*>(a.logits) + row * a.ld, first, end, a.vec, [&](float v, int) {
+  const SampleAsk ask = sample_ask(a, row, sample_row_top(w, row, group));      // (its barrier is the histogram's too)
+  if (!ask.draw) return;                                  // uniform
+  values.each([&](float v, int) {
     const u64_t add = ask.k ? 1 : sample_weight(v, ask.most, ask.per);
     if (add) atomicAdd(&hist[sample_step(v, ask.most)], add);
   });
@@ -293,294 +334,320 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(Sample
     if (hist[i]) atomicAdd(&w.hist[(long)row * kSampleSteps + i], hist[i]);
 }
 
-// What the histogram says of a row.
-struct SampleBorder {
-  u64_t target, before;                                   // counts or weights: what is to be reached, and what lies above the bin
-  int bin;                                                // kSampleSteps: everything is kept
-};
-// by a whole work-group of `threads`; part: threads / 64 + 3 words of LDS
-__device__ __forceinline__ SampleBorder sample_border(const SampleWork& w, const SampleAsk& ask, int row, u64_t* part, int threads) {
-  const int each = bpdq_ceil_div(kSampleSteps, threads), waves = threads / 64, tid = threadIdx.x;
-  const u64_t* hist = w.hist + (long)row * kSampleSteps;
-  u64_t mine = 0;
-  for (int e = 0; e < each; ++e)
-    if (tid * each + e < kSampleSteps) mine += hist[tid * each + e];
-  u64_t run = mine;
+// where the histogram reaches its target, by a whole work-group; found: two words of LDS
+__device__ __forceinline__ SampleBorder sample_border(const SampleWork& w, const SampleAsk& ask, int row, u64_t top, SampleChunkGroup& group,
+                                                      u64_t* found) {
+  constexpr int kEach = kSampleSteps / kSampleChunkThreads;
+  static_assert(kEach * kSampleChunkThreads == kSampleSteps, "whole shares");
+  u64_t hist[kEach], mine = 0, total;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64_t b = __shfl_up(run, o, 64);
-    if ((tid & 63) >= o) run += b;
-  }
-  __syncthreads();
-  if ((tid & 63) == 63) part[tid >> 6] = run;
-  if (tid == 0) part[waves] = kSampleSteps;
-  __syncthreads();
-  u64_t total = 0;
-  for (int q = 0; q < waves; ++q) {
-    if (q == tid >> 6) run += total;
-    total += part[q];
-  }
+  for (int e = 0; e < kEach; ++e) hist[e] = w.hist[(long)row * kSampleSteps + threadIdx.x * kEach + e];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) mine += hist[e];
+  if (threadIdx.x == 0) found[0] = kSampleSteps;
+  const u64_t run = group.scan(mine, total);
   SampleBorder s;
+  s.top = top;
   s.target = ask.k ? (u64_t)ask.k : sample_share(ask.p, total, true);
   if (s.target == 0) s.target = 1;
-  if (run >= s.target && run - mine < s.target) {
-    u64_t before = run - mine;
-    for (int e = 0; e < each; ++e) {
-      const u64_t here = hist[tid * each + e];
-      if (before + here >= s.target) {
-        part[waves] = tid * each + e;
-        part[waves + 1] = before;
-        break;
+  u64_t before = run - mine;
+  if (run >= s.target && before < s.target) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      if (before < s.target && before + hist[e] >= s.target) {
+        found[0] = threadIdx.x * kEach + e;
+        found[1] = before;
       }
-      before += here;
+      before += hist[e];
     }
   }
   __syncthreads();
-  s.bin = (int)part[waves];
-  s.before = s.bin < kSampleSteps ? part[waves + 1] : 0;
+  s.bin = found[0];
+  s.before = s.bin < kSampleSteps ? found[1] : 0;
   return s;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(SampleArgs a, SampleWork w) {
-  __shared__ u64_t part[kSampleChunkThreads / 64 + 2];
+  __shared__ u64_t part[2][kSampleChunkThreads / 64], found[2];
   __shared__ u64_t list[kSampleList];
   __shared__ int count, from;
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, first = chunk * w.turns * kSampleTurn;
-  const int end = first + w.turns * kSampleTurn < a.n_vocab ? first + w.turns * kSampleTurn : a.n_vocab;
-  const SampleAsk ask = sample_ask(a, row, sample_row_top(w, row, part));
-  if (!ask.draw) return;                                  // uniform
-  int bin = kSampleSteps;
-  if (ask.k || ask.p < 1.f) bin = sample_border(w, ask, row, part, kSampleChunkThreads).bin;
-  const bool all = ask.k && ask.p < 1.f;                  // the whole top-k goes to the list
+  SampleChunkGroup group(part);
+  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks;
+  SampleChunk<T> values(a, w, row, chunk);
   if (threadIdx.x == 0) count = 0;
-  __syncthreads();
+  const u64_t top = sample_row_top(w, row, group);
+  const SampleAsk ask = sample_ask(a, row, top);
+  SampleBorder border = {top, 0, 0, kSampleSteps};
+  if (ask.draw && (ask.k || ask.p < 1.f)) border = sample_border(w, ask, row, top, group, found);       // uniform
+  if (chunk == 0 && threadIdx.x == 0) w.border[row] = border;
+  if (!ask.draw) return;                                  // uniform
+  const int bin = (int)border.bin;
+  const bool all = ask.k && ask.p < 1.f;                  // the whole top-k goes to the list
   u64_t sum = 0;
-  sample_each(a, static_cast<const T*>(a.logits) + row * a.ld, first, end, a.vec, [&](float v, int i) {
-    const int step = bin < kSampleSteps ? sample_step(v, ask.most) : 0;
-    if (step > bin) return;
-    if (bin < kSampleSteps && (all || step == bin)) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kSampleList) list[at] = (u64_t)sample_key(v) << 32 | (uint32_t)~i;
-      return;
+  values.each([&](float v, int i) {
+    if (bin < kSampleSteps) {                             // uniform
+      const int step = sample_step(v, ask.most);
+      if (step > bin) return;
+      if (all || step == bin) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kSampleList) list[at] = sample_place(sample_key(v), i);
+        return;
+      }
     }
     const u64_t one = sample_weight(v, ask.most, ask.per);
     if (one >= ask.least) sum += one;
   });
-  sum = sample_fold(sum, part, sample_add);
+  sum = group.sum(sum);
   if (threadIdx.x == 0) {
     w.sum[blockIdx.x] = sum;
-    // (a chunk's count is at most 2^20 and a row's 2^20, so the sum with a chunk that did not fit stays above the list's length)
+    // (a row's counts add up to 2^20 at most; with a chunk's that did not fit they stay above the list's length)
     from = count ? atomicAdd(&w.count[row], count) : 0;
   }
+  if (bin == kSampleSteps) return;                        // uniform: no list
   __syncthreads();
   if (from + count <= kSampleList)
     for (int i = threadIdx.x; i < count; i += kSampleChunkThreads) w.list[(long)row * kSampleList + from + i] = list[i];
 }
 
-// the running sum at which the token is
-__device__ __forceinline__ u64_t sample_draw(float u, u64_t total) {
-  const u64_t target = u > 0.f ? sample_share(u < 1.f ? u : 1.f, total, false) + 1 : 1;
-  return target < total ? target : total;
+typedef SampleGroup<kSampleThreads> SampleRowGroup;
+
+struct SampleShared {
+  u64_t hist[kSampleBins];
+  u64_t part[2][kSampleThreads / 64];
+  u64_t before, value, cut;
+  int bin;
+};
+static_assert(kSampleBins == kSampleThreads, "a thread to a bin");
+
+// The first bin, from the top if `down`, where the running sum reaches `target` (>= 1): sh.bin (-1: none), sh.before and sh.value.
+__device__ __forceinline__ void sample_find(SampleShared& sh, SampleRowGroup& group, bool down, u64_t target) {
+  __syncthreads();
+  const int bin = down ? kSampleBins - 1 - (int)threadIdx.x : (int)threadIdx.x;
+  const u64_t mine = sh.hist[bin];
+  u64_t total;
+  if (threadIdx.x == 0) sh.bin = -1;
+  const u64_t run = group.scan(mine, total);
+  if (run >= target && run - mine < target) {
+    sh.bin = bin;
+    sh.before = run - mine;
+    sh.value = mine;
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void sample_clear(SampleShared& sh) {
+  __syncthreads();
+  sh.hist[threadIdx.x] = 0;
+  __syncthreads();
 }
 
 // A row by one work-group: every selection by radix, passes over the row itself.
 template <typename T>
-__device__ __noinline__ void sample_row(const SampleArgs& a, const SampleAsk& ask, int row, SampleShared& sh) {
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const SampleAsk& ask, int row, SampleShared& sh, SampleRowGroup& group) {
   const int tid = threadIdx.x;
   const T* x = static_cast<const T*>(a.logits) + row * a.ld;
-  auto each = [&](auto f) {
-    for (int i = tid; i < a.n_vocab; i += kSampleThreads) {
-      const uint32_t key = sample_key((float)x[i]);
-      if (key) f(key, i);
+  const int skew = sample_skew(x);
+  auto each = [&](auto f) {                               // f(key, index) of what is there
+    for (int at = 8 * tid - skew; at < a.n_vocab; at += 8 * kSampleThreads) {
+      SampleEight<T> eight;
+      eight.load(x, at, a.n_vocab);
+      eight.each(at, [&](float v, int i) { f(sample_key(v), i); });
     }
   };
-
-  u64_t live = 0;
-  each([&](uint32_t, int) { ++live; });
-  live = sample_sum(sh, live);
   auto weight = [&](uint32_t key) { return sample_weight(sample_value(key), ask.most, ask.per); };
 
-  // kept: keys above tau, and of those at tau the ones up to index last
-  uint32_t tau = 1;
-  int last = a.n_vocab;
-  auto kept = [&](uint32_t key, int i) { return key > tau || (key == tau && i <= last); };
-  // of the kept ones with key t, all but the first n go: last becomes the index of the n-th
-  auto cut = [&](uint32_t t, u64_t n) {
-    int block = 0;
-    for (int step = 0; step < 2; ++step) {
+  // Kept: places from `cut` on.  The place at which the sum of amount(key) over the kept ones, from the largest on, reaches `target`; 0 if it
+  // does not.
+  u64_t cut = 0;
+  auto select = [&](u64_t target, auto amount) {
+    u64_t prefix = 0;
+    constexpr int kBits = 10;
+    static_assert(kSampleBins == 1 << kBits, "digits");
+    for (int shift = 5 * kBits; shift >= 0; shift -= kBits) {       // 52 bits of a place
       sample_clear(sh);
       each([&](uint32_t key, int i) {
-        if (key == t && kept(key, i) && (step == 0 || i / kSampleBins == block))
-          atomicAdd(&sh.hist[step == 0 ? i / kSampleBins : i % kSampleBins], 1ull);
+        const u64_t place = sample_place(key, i);
+        if (place >= cut && place >> (shift + kBits) == prefix) atomicAdd(&sh.hist[place >> shift & (kSampleBins - 1)], amount(key));
       });
-      sample_find(sh, kSampleBins, false, n);
-      n -= sh.before;
-      if (step == 0) block = sh.bin;
-    }
-    return block * kSampleBins + sh.bin;
-  };
-  // The key at which the sum of amount(key) over the kept ones, from the largest on, reaches `target`: its value in sh.value, what is above in `above`.
-  auto select = [&](u64_t target, u64_t& above, auto amount) {
-    uint32_t prefix = 0;
-    above = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      sample_clear(sh);
-      each([&](uint32_t key, int i) {
-        if (kept(key, i) && (shift == 24 || key >> (shift + 8) == prefix)) atomicAdd(&sh.hist[key >> shift & 255], amount(key));
-      });
-      sample_find(sh, 256, true, target - above);
-      above += sh.before;
-      prefix = prefix << 8 | (uint32_t)sh.bin;
+      sample_find(sh, group, true, target);
+      if (sh.bin < 0) return (u64_t)0;                    // uniform
+      target -= sh.before;
+      prefix = prefix << kBits | (u64_t)sh.bin;
     }
     return prefix;
   };
 
-  const int k = ask.k;
-  if (k > 0 && (u64_t)k < live) {
-    u64_t above;
-    const uint32_t t = select((u64_t)k, above, [](uint32_t) { return 1ull; });
-    const int at = (u64_t)k - above < sh.value ? cut(t, (u64_t)k - above) : last;
-    tau = t;
-    last = at;
-  }
+  if (ask.k) cut = select((u64_t)ask.k, [](uint32_t) { return 1ull; });
   if (ask.p < 1.f) {
     u64_t total = 0;
     each([&](uint32_t key, int i) {
-      if (kept(key, i)) total += weight(key);
+      if (sample_place(key, i) >= cut) total += weight(key);
     });
-    total = sample_sum(sh, total);
-    u64_t target = sample_share(ask.p, total, true), above;
-    if (target == 0) target = 1;
-    const uint32_t t = select(target, above, weight);
-    const u64_t one = weight(t), n = (target - above + one - 1) / one;
-    const int at = n * one < sh.value ? cut(t, n) : t == tau ? last : a.n_vocab;
-    tau = t;
-    last = at;
+    const u64_t target = sample_share(ask.p, group.sum(total), true);
+    cut = select(target > 0 ? target : 1, weight);
   }
-  // the draw
+  // the draw: a digit of the index, then the next
   int block = 0;
-  u64_t total = 0, target = 0, value = 0;
+  u64_t total = 0, target = 0;
   for (int step = 0; step < 2; ++step) {
     sample_clear(sh);
     u64_t sum = 0;
     each([&](uint32_t key, int i) {
-      if (!kept(key, i) || (step == 1 && i / kSampleBins != block)) return;
+      if (sample_place(key, i) < cut || (step == 1 && i / kSampleBins != block)) return;
       const u64_t w = weight(key);
       if (w < ask.least) return;
       atomicAdd(&sh.hist[step == 0 ? i / kSampleBins : i % kSampleBins], w);
       sum += w;
     });
     if (step == 0) {
-      total = sample_sum(sh, sum);
+      total = group.sum(sum);
       target = sample_draw(a.u[row], total);
     }
-    sample_find(sh, kSampleBins, false, target);
+    sample_find(sh, group, false, target);
     target -= sh.before;
-    value = sh.value;
     if (step == 0) block = sh.bin;
   }
   if (tid == 0) {
     a.token[row] = block * kSampleBins + sh.bin;
-    if (a.prob) a.prob[row] = (float)((double)value / (double)total);
+    if (a.prob) a.prob[row] = (float)((double)sh.value / (double)total);
   }
 }
-
 
 template <typename T>
 __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs a, SampleWork w) {
   __shared__ SampleShared sh;
-  __shared__ u64_t list[kSampleList], weights[kSampleList];
-  static_assert(kSampleChunks <= kSampleBins && kSampleThreads >= kSampleChunks, "a row's chunks are a histogram's bins");
+  SampleRowGroup group(sh.part);
+  constexpr int kEach = kSampleList / kSampleThreads;
   const int tid = threadIdx.x, row = blockIdx.x;
-  const u64_t top = sample_max(sh, tid < w.chunks ? w.top[(long)row * w.chunks + tid] : 0);
-  const SampleAsk ask = sample_ask(a, row, top);
+  const SampleBorder border = w.border[row];
+  const SampleAsk ask = sample_ask(a, row, border.top);
   if (!ask.draw) {                                        // uniform: nothing is there, or the largest is asked for
     if (tid == 0) {
-      a.token[row] = top ? (int)~(uint32_t)top : -1;
-      if (a.prob) a.prob[row] = top ? 1.f : 0.f;
+      a.token[row] = border.top ? sample_index(border.top) : -1;
+      if (a.prob) a.prob[row] = border.top ? 1.f : 0.f;
     }
     return;
   }
-  u64_t cut = 0;
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  const int skew = sample_skew(x), span = w.turns * kSampleTurn;
+  const bool both = ask.k && ask.p < 1.f;
+  const int n = border.bin < kSampleSteps ? w.count[row] : 0;
+  // (a top-k that keeps everything before a top-p has no histogram of weights)
+  if (n > kSampleList || (border.bin == kSampleSteps && both)) {       // uniform
+    sample_row<T>(a, ask, row, sh, group);
+    return;
+  }
   sh.hist[tid] = tid < w.chunks ? w.sum[(long)row * w.chunks + tid] : 0;
-  if (ask.k || ask.p < 1.f) {
-    const SampleBorder border = sample_border(w, ask, row, sh.part, kSampleThreads);
-    const int n = border.bin < kSampleSteps ? w.count[row] : 0;
-    // a top-k that keeps everything before a top-p has no histogram of weights
-    if (n > kSampleList || (border.bin == kSampleSteps && ask.k && ask.p < 1.f)) {
-      sample_row<T>(a, ask, row, sh);
-      return;
+  u64_t cut = 0;
+  if (n > 0) {
+    // the list, in registers
+    u64_t place[kEach], weight[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+      const int i = tid + q * kSampleThreads;
+      place[q] = i < n ? w.list[(long)row * kSampleList + i] : 0;
+      weight[q] = i < n ? sample_weight(sample_value(sample_key_of(place[q])), ask.most, ask.per) : 0;
     }
-    for (int i = tid; i < n; i += kSampleThreads) {
-      list[i] = w.list[(long)row * kSampleList + i];
-      weights[i] = sample_weight(sample_value((uint32_t)(list[i] >> 32)), ask.most, ask.per);
+    if (n <= 64) {
+      // one wavefront: everyone's rank and the weight above
+      if (tid < 64) {
+        u64_t above = 0;
+        int rank = 0;
+        for (int j = 0; j < n; ++j) {
+          const bool larger = sample_lane(place[0], j) > place[0];
+          rank += larger;
+          above += larger ? sample_lane(weight[0], j) : 0;
+        }
+        bool in = tid < n;
+        if (both) {                                       // top-p of the exact top-k
+          in = in && rank < ask.k;
+          const u64_t total = sample_lane(sample_wave_scan<false>(in ? weight[0] : 0), 63), target = sample_share(ask.p, total, true);
+          in = in && above < (target > 0 ? target : 1);
+        } else {
+          in = in && border.before + (ask.k ? (u64_t)rank : above) < border.target;
+        }
+        const u64_t last = sample_lane(sample_wave_scan<true>(in ? ~place[0] : 0), 63);
+        if (tid == 0) sh.cut = ~last;
+      }
+    } else {
+      // The place at which the running sum over the list, from the largest on, reaches `target`: 1024 bins over what is left of its range at
+      // a time, until a bin holds one.
+      u64_t low = 0, high = 0;
+#pragma unroll
+      for (int q = 0; q < kEach; ++q) {
+        if (place[q]) low = low > ~place[q] ? low : ~place[q];
+        high = high > place[q] ? high : place[q];
+      }
+      low = ~group.max(low);
+      high = group.max(high);
+      const u64_t mine = tid < w.chunks ? sh.hist[tid] : 0;
+      auto select = [&](u64_t target, u64_t from, bool count) {
+        u64_t lo = low > from ? low : from, hi = high;
+        for (;;) {
+          const int bits = 64 - __clzll((long long)(hi - lo)), shift = hi == lo || bits <= 10 ? 0 : bits - 10;
+          sample_clear(sh);
+#pragma unroll
+          for (int q = 0; q < kEach; ++q)
+            if (place[q] >= lo && place[q] <= hi) atomicAdd(&sh.hist[(place[q] - lo) >> shift], count ? 1ull : weight[q]);
+          sample_find(sh, group, true, target);
+          if (sh.bin < 0) return lo;                      // (cannot be: the histogram counted these)
+          target -= sh.before;
+          lo += (u64_t)sh.bin << shift;
+          const u64_t end = lo + ((1ull << shift) - 1);
+          hi = hi < end ? hi : end;
+          int in = 0;
+#pragma unroll
+          for (int q = 0; q < kEach; ++q) in += place[q] >= lo && place[q] <= hi;
+          if (shift == 0 || (__syncthreads_count(in > 0) <= 1 && !__syncthreads_or(in > 1))) return lo;
+        }
+      };
+      if (both) {
+        cut = select((u64_t)ask.k, 0, true);
+        u64_t total = 0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+          if (place[q] >= cut) total += weight[q];
+        const u64_t target = sample_share(ask.p, group.sum(total), true);
+        cut = select(target > 0 ? target : 1, cut, false);
+      } else {
+        cut = select(border.target - border.before, 0, ask.k != 0);
+      }
+      __syncthreads();
+      sh.hist[tid] = mine;
+      if (tid == 0) sh.cut = cut;
     }
     __syncthreads();
-    // ranks in the list, and the weight above
-    constexpr int kEach = kSampleList / kSampleThreads;
-    int rank[kEach];
-    u64_t above[kEach];
+    cut = sh.cut;
 #pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-      rank[q] = 0;
-      above[q] = 0;
-      const int i = tid + q * kSampleThreads;
-      if (i >= n) continue;
-      const u64_t mine = list[i];
-      for (int j = 0; j < n; ++j)
-        if (list[j] > mine) {
-          ++rank[q];
-          above[q] += weights[j];
-        }
-    }
-    u64_t target = border.target, before = border.before;
-    const bool all = ask.k && ask.p < 1.f;
-    if (all) {                                            // of the exact top-k
-      u64_t total = 0;
-#pragma unroll
-      for (int q = 0; q < kEach; ++q)
-        if (tid + q * kSampleThreads < n && rank[q] < ask.k) total += weights[tid + q * kSampleThreads];
-      total = sample_sum(sh, total);
-      target = sample_share(ask.p, total, true);
-      if (target == 0) target = 1;
-      before = 0;
-    }
-    u64_t last = ~0ull;
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-      const int i = tid + q * kSampleThreads;
-      if (i >= n) continue;
-      const bool in = all ? rank[q] < ask.k && above[q] < target : ask.k ? before + rank[q] < target : before + above[q] < target;
-      if (!in) continue;
-      last = last < list[i] ? last : list[i];
-      if (weights[i] >= ask.least) atomicAdd(&sh.hist[(int)~(uint32_t)list[i] / (w.turns * kSampleTurn)], weights[i]);
-    }
-    cut = ~sample_max(sh, ~last);                         // the smallest of the kept ones
-    if (border.bin == kSampleSteps) cut = 0;
+    for (int q = 0; q < kEach; ++q)
+      if (place[q] >= cut && weight[q] >= ask.least)      // (an empty place has no weight)
+        atomicAdd(&sh.hist[(sample_index(place[q]) + skew) / span], weight[q]);
   }
   __syncthreads();
-  u64_t total = sample_sum(sh, sh.hist[tid]);
+  // the chunk, and in it a thread's consecutive values
+  u64_t total, run, mine = sh.hist[tid];
+  run = group.scan(mine, total);
   u64_t target = sample_draw(a.u[row], total);
-  sample_find(sh, w.chunks, false, target);
+  if (run >= target && run - mine < target) {
+    sh.bin = tid;
+    sh.before = run - mine;
+  }
+  __syncthreads();
   target -= sh.before;
-  // in the chunk: a thread's consecutive values
-  const int span = w.turns * kSampleTurn, each = span / kSampleThreads, first = sh.bin * span + tid * each;
-  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  const int each = span / kSampleThreads, first = sh.bin * span + tid * each - skew;
   auto one = [&](int i) -> u64_t {
-    if (i >= a.n_vocab) return 0;
+    if (i < 0 || i >= a.n_vocab) return 0;
     const uint32_t key = sample_key((float)x[i]);
-    if (key == 0 || ((u64_t)key << 32 | (uint32_t)~i) < cut) return 0;
+    if (key == 0 || sample_place(key, i) < cut) return 0;
     const u64_t v = sample_weight(sample_value(key), ask.most, ask.per);
     return v >= ask.least ? v : 0;
   };
-  u64_t mine = 0;
+  mine = 0;
   for (int e = 0; e < each; ++e) mine += one(first + e);
-  __syncthreads();
-  sh.hist[tid] = mine;
-  sample_find(sh, kSampleThreads, false, target);
-  if (tid == sh.bin) {
-    u64_t run = sh.before;
+  u64_t here;
+  run = group.scan(mine, here);
+  if (run >= target && run - mine < target) {
+    run -= mine;
     for (int e = 0; e < each; ++e) {
       const u64_t v = one(first + e);
       run += v;
@@ -642,8 +709,7 @@ extern "C" int bpdq_sample(const void* logits, int n_tok, int n_vocab, long ldl,
   const size_t need = bpdq_sample_workspace_bytes(n_tok, n_vocab);
   if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255))) return -13;
   if (ws_bytes < need) return -14;
-  const int vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && (size_t)ldl * (dtype == BPDQ_F32 ? 4 : 2) % 16 == 0;
-  const SampleArgs a = {logits, u, temperature, top_k, top_p, min_p, token, prob, ldl, n_tok, n_vocab, vec};
+  const SampleArgs a = {logits, u, temperature, top_k, top_p, min_p, token, prob, ldl, n_tok, n_vocab};
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (dtype == BPDQ_F32) return sample_launch<float>(a, ws, stream);
   if (dtype == BPDQ_F16) return sample_launch<_Float16>(a, ws, stream);
