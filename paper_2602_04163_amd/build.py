@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libbpdq.so")
 SOURCES = ["linear_k4.hip", "gated_k4.hip", "linear_k3.hip", "gated_k3.hip", "linear_k2.hip", "gated_k2.hip", "linear_k1.hip", "gated_k1.hip", "group_sweep_k3_g256.hip",
            "group_sweep_k3_g256u.hip", "group_sweep_k2_g256.hip", "group_sweep_k2_g256u.hip",
            "group_sweep_k1_g256.hip", "group_sweep_k1_g256u.hip", "group_sweep_k4.hip",
-           "group_sweep_k3.hip", "group_sweep_k2.hip", "group_sweep_k1.hip", "hessian.hip", "prepare.hip", "quantize.hip", "order.hip", "gemv.hip", "linear.hip",
+           "group_sweep_k3.hip", "group_sweep_k2.hip", "group_sweep_k1.hip", "hessian.hip", "prepare.hip", "quantize.hip", "order.hip", "gemv.hip", "gated_token.hip", "linear.hip",
            "kv_attention.hip", "kv_cache.hip", "sample.hip", "norm.hip", "rotary.hip", "ceilings.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,147 @@
+// The gated product (linear.h) for one token: the look-ups of gemv.hip, gate and up row of a value by the same wavefront.
+//
+// What bounds it: the look-ups' vector instructions and LDS reads beside the memory, as there.  Against the few-token kernel of the matrix
+// instructions, which decodes weights that one token uses once.
+#include "gemv.h"
+#include "linear.h"
+
+namespace bpdq {
+
+// One chunk: d_in <= 2048 W.  ROWS = 2: an item is both rows; 1: an item is one of them, the gate's first.
+template <int K, int W, int NG, int ROWS, bool STRIDED>
+__global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a, int bf16, int passes) {
+  extern __shared__ float lds[];
+  float* T = lds;                                        // [8][W][16][64], at LDS address 0: the kernel has no other LDS
+  float* Sw = lds + 8 * W * 16 * 64;                     // [W][64]: sum of x over each word
+  constexpr int kSegs = 8 * W, kSegPerThread = (kSegs + kGemvWaves - 1) / kGemvWaves;
+  const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32, half = a.d_out / 2;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int step = gridDim.x * kGemvWaves, first = blockIdx.x * kGemvWaves + wave;
+  constexpr int kItems = 3 - ROWS;                       // of a pair of rows
+  typedef GemvItem<K, W, NG, ROWS, !STRIDED && (NG > 1)> Item;
+  Item cur, nxt;
+  const GemvPlace<W, STRIDED> at(0, nw, wpg, lane);
+  auto fetch = [&](int item, Item& it) {
+    int f = first + item / kItems * step;
+    f = f < half ? f : half - 1;
+    gemv_fetch<K, W, NG, ROWS, STRIDED, true>(a.planes, a.coefs, a.d_out, nw, n_grp, wpg, f + (ROWS == 1 && item % 2 ? half : 0), 0, nw, lane,
+                                              at, it);
+  };
+  // x of the table's segments: bf16 under 2^-24, so that sums of its largest values stay finite
+  const unsigned short* x = static_cast<const unsigned short*>(a.x);
+  float4 xv[kSegPerThread];
+#pragma unroll
+  for (int s = 0; s < kSegPerThread; ++s) {
+    const int id = wave + kGemvWaves * s;                // segment (q, j) = (id / W, id % W)
+    const int wl = STRIDED ? 64 * (id % W) + lane : W * lane + id % W;
+    const bool in = id < kSegs && wl < nw;
+    const unsigned short* p = x + (in ? 32 * wl + 4 * (id / W) : 0);
+    unsigned short h[4];
+    if (a.vec_x) *reinterpret_cast<uint2*>(h) = *reinterpret_cast<const uint2*>(p);
+    else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = p[e];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = bf16 ? __builtin_bit_cast(float, (uint32_t)h[e] << 16) * 0x1p-24f : (float)__builtin_bit_cast(_Float16, h[e]);
+      v[e] = in ? v[e] : 0.f;
+    }
+    xv[s] = make_float4(v[0], v[1], v[2], v[3]);
+  }
+  fetch(0, cur);
+#pragma unroll
+  for (int s = 0; s < kSegPerThread; ++s) {
+    const int id = wave + kGemvWaves * s;
+    if (id < kSegs) gemv_table(xv[s], T + id * 16 * 64 + lane);
+  }
+  __syncthreads();
+  if (tid < 64 * W) {
+    float sw = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sw += T[((q * W + (tid >> 6)) * 16 + 15) * 64 + lane];
+    Sw[tid] = sw;
+  }
+  __syncthreads();
+  // the first item is here: or the look-ups below, reached with and without a request ahead of them, would wait for
+  // everything in flight (vmcnt 0; the other counters at their maxima)
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  float gate = 0.f;
+  for (int item = 0; item < passes * kItems; ++item) {
+    const int f = first + item / kItems * step;
+    if (f >= half) break;                                // uniform over the wavefront
+    if (item + 1 < passes * kItems) fetch(item + 1, nxt);
+    float v[ROWS];
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) v[q] = gemv_row<K, W, NG, STRIDED>(cur, q, Sw, nw, lane);
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q)
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) v[q] += __shfl_xor(v[q], o, 64);
+    cur = nxt;
+    if (ROWS == 1 && item % 2 == 0) {
+      gate = v[0];
+      continue;
+    }
+    float up = v[ROWS - 1];
+    if (ROWS == 2) gate = v[0];
+    if (bf16) {
+      gate *= 0x1p24f;
+      up *= 0x1p24f;
+    }
+    if (lane == 0) {
+      if (a.bias) {
+        const unsigned short g = static_cast<const unsigned short*>(a.bias)[f], u = static_cast<const unsigned short*>(a.bias)[half + f];
+        gate += bf16 ? __builtin_bit_cast(float, (uint32_t)g << 16) : (float)__builtin_bit_cast(_Float16, g);
+        up += bf16 ? __builtin_bit_cast(float, (uint32_t)u << 16) : (float)__builtin_bit_cast(_Float16, u);
+      }
+      const float y = linear_act(gate, a.act) * up;
+      if (bf16) static_cast<__bf16*>(a.y)[f] = (__bf16)y;
+      else static_cast<_Float16*>(a.y)[f] = (_Float16)y;
+    }
+  }
+}
+
+// Items of both rows where two of them, this one and the next, fit the 128 registers of a 1024-thread work-group.
+template <int K, int W, int NG, bool STRIDED>
+static int gated_token_launch(const LinearArgs& a, int bf16, hipStream_t stream) {
+  constexpr int kRegs = K * W + (K + 1) * (!STRIDED && NG > 1 ? NG / 2 : NG), ROWS = kRegs <= 21 ? 2 : 1;
+  BPDQ_HIP_TRY((bpdq_lds_limit<&gated_token_kernel<K, W, NG, ROWS, STRIDED>>(gemv_lds_bytes<W>())));
+  const int units = bpdq_ceil_div(a.d_out / 2, kGemvWaves), passes = bpdq_ceil_div(units, 256);
+  hipLaunchKernelGGL((gated_token_kernel<K, W, NG, ROWS, STRIDED>), dim3(bpdq_ceil_div(units, passes)), dim3(kGemvThreads),
+                     gemv_lds_bytes<W>(), stream, a, bf16, passes);
+  BPDQ_LAUNCH_CHECK();
+  return 0;
+}
+
+// Words of a lane as in gemv.hip's rule.
+template <int K>
+static int gated_token_pick(const LinearArgs& a, int bf16, hipStream_t stream) {
+  const int nw = a.d_in / 32, wpg = a.group / 32;
+  if (nw <= 64) return gated_token_launch<K, 1, 1, false>(a, bf16, stream);
+  const int W = nw <= 128 ? 2 : 4, strided = bpdq_ceil_div(nw, 64);
+  const bool idle = 8 * strided <= ((K >= 3 || wpg == 1) ? 6 : 5) * W;
+  const int per = wpg < W ? W / wpg : 1;                 // groups to a lane
+  const bool whole = nw % W == 0 && (wpg % W == 0 || W % wpg == 0) && reinterpret_cast<uintptr_t>(a.planes) % (4 * W) == 0 &&
+                     reinterpret_cast<uintptr_t>(a.coefs) % (2 * per) == 0;
+  if (W == 2) {
+    if (!whole || idle) return gated_token_launch<K, 2, 2, true>(a, bf16, stream);
+    return per == 1 ? gated_token_launch<K, 2, 1, false>(a, bf16, stream) : gated_token_launch<K, 2, 2, false>(a, bf16, stream);
+  }
+  if (!whole || idle) return gated_token_launch<K, 4, 4, true>(a, bf16, stream);
+  return per == 1   ? gated_token_launch<K, 4, 1, false>(a, bf16, stream)
+         : per == 2 ? gated_token_launch<K, 4, 2, false>(a, bf16, stream)
+                    : gated_token_launch<K, 4, 4, false>(a, bf16, stream);
+}
+
+int gated_token_run(const LinearArgs& a, int bits, int bf16, hipStream_t stream) {
+  switch (bits) {
+    case 1: return gated_token_pick<1>(a, bf16, stream);
+    case 2: return gated_token_pick<2>(a, bf16, stream);
+    case 3: return gated_token_pick<3>(a, bf16, stream);
+    default: return gated_token_pick<4>(a, bf16, stream);
+  }
+}
+
+}  // namespace bpdq

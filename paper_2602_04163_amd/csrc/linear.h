@@ -844,6 +844,10 @@ int linear_run(const LinearArgs& a, int dtype, hipStream_t stream) {
   return dtype == BPDQ_F16 ? linear_pick<_Float16, K, GATED>(a, stream) : linear_pick<__bf16, K, GATED>(a, stream);
 }
 
+// the gated product for one token and d_in <= kGatedTokenMost (gated_token.hip)
+constexpr int kGatedTokenMost = 8192;
+int gated_token_run(const LinearArgs& a, int bits, int bf16, hipStream_t stream);
+
 // instantiated in linear_k1.hip to linear_k4.hip, and gated_k1.hip to gated_k4.hip
 extern template int linear_run<1, false>(const LinearArgs&, int, hipStream_t);
 extern template int linear_run<2, false>(const LinearArgs&, int, hipStream_t);

@@ -100,6 +100,7 @@ extern "C" int bpdq_gated_linear(const uint32_t* planes, const uint16_t* coefs_h
   a.vec_w = reinterpret_cast<uintptr_t>(planes) % 16 == 0 && d_in % 128 == 0;
   a.vec_y = reinterpret_cast<uintptr_t>(Y) % 16 == 0 && ldy % 8 == 0;
   hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (n_tok == 1 && d_in <= kGatedTokenMost) return gated_token_run(a, bits, dtype == BPDQ_BF16, stream);
   switch (bits) {
     case 1: return linear_run<1, true>(a, dtype, stream);
     case 2: return linear_run<2, true>(a, dtype, stream);

@@ -328,6 +328,38 @@ def test_gated_kernels(dev, n, d_in, f, bits, group, kind):
     _check_gated(bq.bpdq_gated_linear(p, c, group, x, bias=b), planes, coefs, group, x, b, "silu", kind)
 
 
+# columns and groups for which each form of the one-token kernel is chosen: one, two or four words to a lane, consecutive (sharing one group, two, four)
+# and strided; below and above 256 rows of work-groups
+@pytest.mark.parametrize("d_in,group", [(32, 32), (2048, 64), (2080, 32), (4096, 128), (4096, 32), (3584, 128), (4160, 32), (5120, 64), (8192, 128), (8192, 64),
+                                        (8192, 32), (8160, 96), (6176, 32), (8224, 32)])
+@pytest.mark.parametrize("bits,kind,f,bias", [(1, "f16", 300, True), (2, "bf16", 5000, False), (3, "f16", 17, False), (4, "bf16", 4100, True)])
+def test_gated_token(dev, d_in, group, bits, kind, f, bias):
+    print(f"gated token k={bits} g={group} 2x{f}x{d_in} {kind}", flush=True)
+    planes, coefs = _layer(2 * f, d_in, bits, group, d_in + f)
+    g = torch.Generator().manual_seed(d_in)
+    x = (torch.randn((1, d_in), generator=g) * torch.exp(0.5 * torch.randn(d_in, generator=g))).to(TYPES[kind]).to(dev)
+    b = torch.randn(2 * f, generator=g).to(TYPES[kind]).to(dev) if bias else None
+    p, c = _on(planes, coefs, dev)
+    y = bq.bpdq_gated_linear(p, c, group, x, bias=b)
+    _check_gated(y, planes, coefs, group, x, b, "silu", kind)
+    into = _inside(torch.zeros((1, f), dtype=x.dtype, device=dev), f + 3, 1)
+    bq.bpdq_gated_linear(p, c, group, _inside(x, d_in + 1, 1), bias=b, Y=into)
+    assert torch.equal(into, y)
+
+
+def test_gated_token_magnitudes(dev):
+    """Sums of the largest values of the type, with and without an infinity."""
+    planes, coefs = _layer(2 * 40, 256, 2, 64, 7)
+    p, c = _on(planes, coefs * np.float16(2.0 ** -6), dev)
+    x = torch.full((1, 256), 2.0 ** 127, dtype=torch.bfloat16, device=dev)
+    want, (gate, up), _, _ = do.gated(planes, coefs * np.float16(2.0 ** -6), 64, _np(x), None, "none")
+    assert np.isfinite(want).all() and np.abs(gate).max() > 2.0 ** 120
+    y = bq.bpdq_gated_linear(p, c, 64, x, act="relu")
+    assert (_np(y)[np.abs(want) > 2.0 ** 129] != 0).any() and not y.isnan().any()
+    x[0, 3] = INF
+    assert not bq.bpdq_gated_linear(p, c, 64, x, act="none").isfinite().all()
+
+
 @pytest.mark.parametrize("n", [3, 40])
 def test_gated_strides_and_infinities(dev, n):
     planes, coefs = _layer(2 * 70, 320, 2, 64, 5)
