@@ -332,6 +332,13 @@ __device__ __forceinline__ f32x16_t mfma_32x32x16(u32x4_t a, u32x4_t b, f32x16_t
 __device__ __forceinline__ void lds_dma_1k(const void* base, unsigned voff, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
 }
+// The same with 4 bytes a lane, and with 2, which are zero-extended to 4.
+__device__ __forceinline__ void lds_dma_dword(const void* base, unsigned voff, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+}
+__device__ __forceinline__ void lds_dma_ushort(const void* base, unsigned voff, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory");
+}
 // Waits until at most N vector-memory operations are outstanding (the other counters' fields at their maxima).
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -348,10 +355,14 @@ struct LinearTile {
   static constexpr int kAcc = 16 * RT * TT;              // accumulators of a lane
   static constexpr int kDma = kToks * 128 / 1024 / (WR * WT);       // requests of a wavefront per 64 columns
   static constexpr int kStage = kToks * 128;             // bytes of 64 columns of X
-  static constexpr int kLevel = 8 * PlaneLevels<K>::kRegs;        // bytes of the levels of a row and group
-  static constexpr int kTable = 2 * kRows * kLevel;      // of the rows' levels of a stage, one word for each half
   static constexpr int kRing = kStages * KS * kStage;
-  static constexpr size_t kLds = (size_t)kRing + 2 * KS * kTable;
+  // a wavefront's own: the coefficients of a group of its rows, and its words, of four to a lane or, where these do not fit, of one
+  static constexpr int kWaves = kThreads / 64;
+  static constexpr int kCoefs = (K + 1) * RT * 256;
+  static constexpr bool kFour = kRing + kWaves * (kCoefs + K * RT * 1024) <= 160 * 1024;
+  static constexpr int kWordBytes = K * RT * (kFour ? 1024 : 256);
+  static constexpr size_t kLds = (size_t)kRing + kWaves * (kCoefs + kWordBytes);
+  static_assert(WT == 1, "a row belongs to one wavefront of a part");
   static_assert(kDma % 4 == 0, "a quarter with each step");
   static_assert(kStages >= 3, "the requests of a stage are spread over the one before");
   static_assert(kLds <= 160 * 1024, "one work-group to a CU");
@@ -487,7 +498,13 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int tid = threadIdx.x % S::kPart, lane = tid & 63, low = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % S::WR, wt = wave / S::WR;
-  const int row0 = blockIdx.x / tok_tiles * S::kRows, tok0 = blockIdx.x % tok_tiles * S::kToks;
+  // Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own: consecutive tiles, which share rows, go to one XCD.
+  int tile = blockIdx.x;
+  if (tok_tiles % 8 != 0) {
+    const int all = gridDim.x / 8, more = gridDim.x % 8, xcd = tile % 8;
+    tile = xcd * all + (xcd < more ? xcd : more) + tile / 8;
+  }
+  const int row0 = tile / tok_tiles * S::kRows, tok0 = tile % tok_tiles * S::kToks;
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32;
   const int all_chunks = bpdq_ceil_div(nw, 2 * W);
   const int n_chunk = bpdq_ceil_div(all_chunks, S::KS);  // of a part, the last one maybe past the end
@@ -527,77 +544,66 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     const int at = 32 * (RT * wr + r) + low;
     row[r] = stored(at);
   }
-  uint32_t w_cur[RT][K][W], w_next[RT][K][W];
-  auto load_w = [&](int chunk) {                         // words past the end: the row's first, under levels of zero
-    const int word = 2 * W * chunk + W * half;
+  // Words and coefficients go through LDS too, by the wavefront that needs them, so that every load of the loop is a request whose wait is
+  // counted: a load into registers would wait for all requests behind it (the compiler does not count these).
+  constexpr bool kFour = VEC && S::kFour;                // four words at a time (of a chunk), or one (of a stage)
+  constexpr int kW = kFour ? W : 1;
+  const unsigned own = (unsigned)(S::kRing + (part * (S::kPart / 64) + wave) * (S::kCoefs + S::kWordBytes));
+  const char* own_c = lds + own + 4 * lane;
+  const char* own_w = lds + own + S::kCoefs + (kFour ? 16 : 4) * lane;
+  auto level_word = [&](int stage) { return 2 * W * (stage / W * S::KS + part) + W * half + stage % W; };
+  auto request_w = [&](int stage) {                      // words past the end: the row's first, under levels of zero
+    const int word = level_word(stage);
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int i = 0; i < K; ++i) {
-        if constexpr (VEC) {                             // rows are whole lanes
-          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(w_base[i] + (row[r] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u);
-#pragma unroll
-          for (int j = 0; j < W; ++j) w_next[r][i][j] = v[j];
-        } else {
-#pragma unroll
-          for (int j = 0; j < W; ++j)
-            w_next[r][i][j] = *reinterpret_cast<const uint32_t*>(
-                w_base[i] + (row[r] * (unsigned)nw + (unsigned)(word + j < nw ? word + j : 0)) * 4u);
-        }
+        const unsigned voff = (row[r] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u;
+        if constexpr (kFour) lds_dma_1k(w_base[i], voff, own + S::kCoefs + (r * K + i) * 1024);
+        else lds_dma_dword(w_base[i], voff, own + S::kCoefs + (r * K + i) * 256);
       }
   };
-  auto take_w = [&]() {
+  auto request_c = [&](int stage) {                      // of the group that begins with the stage's word
+    const int word = level_word(stage);
+    const unsigned g = (unsigned)(word < nw ? word : 0) / (unsigned)wpg;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int i = 0; i < K; ++i)
-#pragma unroll
-        for (int j = 0; j < W; ++j) w_cur[r][i][j] = w_next[r][i][j];
+      for (int i = 0; i <= K; ++i) lds_dma_ushort(c_base[i], (row[r] * (unsigned)n_grp + g) * 2u, own + (r * (K + 1) + i) * 256);
   };
-
-  // Levels of the stages whose words begin a group: the part's threads make them for all rows, [half][row], from coefficients that
-  // were requested when the levels before them were made.
-  char* table = lds + S::kRing + part * 2 * S::kTable;
-  typedef uint32_t Level __attribute__((ext_vector_type(2 * PlaneLevels<K>::kRegs)));
-  constexpr int kUnits = 2 * S::kRows / S::kPart;        // (half, row) pairs of a thread
-  _Float16 c_raw[kUnits][K + 1];
-  auto level_word = [&](int stage, int h) { return 2 * W * (stage / W * S::KS + part) + W * h + stage % W; };
-  auto load_levels = [&](int stage) {
+  uint32_t w_cur[RT][K][kW], w_next[RT][K][kW];
+  auto read_w = [&](uint32_t (&w)[RT][K][kW]) {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int id = u * S::kPart + tid, r = id % S::kRows, word = level_word(stage, id / S::kRows);
-      const unsigned g = (unsigned)(word < nw ? word : 0) / (unsigned)wpg;
-      const unsigned at = stored(r);
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int i = 0; i <= K; ++i)
-        c_raw[u][i] = *reinterpret_cast<const _Float16*>(c_base[i] + (at * (unsigned)n_grp + g) * 2u);
-    }
-  };
-  auto store_levels = [&](int stage) {
+      for (int i = 0; i < K; ++i) {
+        if constexpr (kFour) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(own_w + (r * K + i) * 1024);
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int id = u * S::kPart + tid;
-      const bool on = level_word(stage, id / S::kRows) < nw;        // words past the end add nothing
-      PlaneLevels<K> made;
-      made.set(c_raw[u]);
-      Level out;
-#pragma unroll
-      for (int n = 0; n < PlaneLevels<K>::kRegs; ++n) {
-        out[2 * n] = on ? made.lo[n] : 0u;
-        out[2 * n + 1] = on ? made.hi[n] : 0u;
+          for (int j = 0; j < W; ++j) w[r][i][j] = v[j];
+        } else {
+          w[r][i][0] = *reinterpret_cast<const uint32_t*>(own_w + (r * K + i) * 256);
+        }
       }
-      reinterpret_cast<Level*>(table + (stage & 1) * S::kTable)[id] = out;
-    }
   };
-  PlaneLevels<K> levels[RT];
-  auto read_levels = [&](int stage) {
+  _Float16 c_raw[RT][K + 1];
+  auto read_c = [&]() {
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i <= K; ++i) c_raw[r][i] = *reinterpret_cast<const _Float16*>(own_c + (r * (K + 1) + i) * 256);
+  };
+  PlaneLevels<K> levels[RT], levels_next[RT];
+  auto make_levels = [&](PlaneLevels<K> (&to)[RT], int stage) {
+    const bool on = level_word(stage) < nw;              // words past the end add nothing
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const Level in = reinterpret_cast<const Level*>(table + (stage & 1) * S::kTable)[half * S::kRows + 32 * (RT * wr + r) + low];
+      PlaneLevels<K> made;
+      made.set(c_raw[r]);
 #pragma unroll
       for (int n = 0; n < PlaneLevels<K>::kRegs; ++n) {
-        levels[r].lo[n] = in[2 * n];
-        levels[r].hi[n] = in[2 * n + 1];
+        to[r].lo[n] = on ? made.lo[n] : 0u;
+        to[r].hi[n] = on ? made.hi[n] : 0u;
       }
     }
   };
@@ -620,45 +626,67 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int r = 0; r < RT; ++r) {
       uint32_t words[K];
 #pragma unroll
-      for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][j];
+      for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][kFour ? j : 0];
       v[f & 1][r] = PlaneWord<K>(words).values(levels[r], f);
     }
   };
 
+  request_w(0);
+  request_c(0);
 #pragma unroll
-  for (int s = 0; s < S::kStages; ++s)
+  for (int s = 0; s < S::kStages - 1; ++s)
 #pragma unroll
-    for (int q = 0; q < (s < S::kStages - 1 ? 4 : 1); ++q) request(s, s, q);
-  load_w(part);
-  load_levels(0);
-  store_levels(0);
-  load_levels(GS);
-  take_w();
-  if (S::kAcc <= 64) load_w(part + S::KS);
-  wait_vm<(S::kStages - 2) * S::kDma + S::kDma / 4>();
-  __syncthreads();
-  read_levels(0);
+    for (int q = 0; q < 4; ++q) request(s, s, q);
+  wait_vm<(S::kStages - 1) * S::kDma>();
+  asm volatile("" ::: "memory");                         // reads of LDS stay behind the wait
+  read_w(w_cur);
+  read_c();
+  make_levels(levels, 0);
+  wait_vm<(S::kStages - 2) * S::kDma>();
+  __syncthreads();                                       // (reads of LDS have their data before it)
+  if (!kFour) request_w(1);
+  request_c(GS);
+  request(S::kStages - 1, S::kStages - 1, 0);
 #pragma unroll
   for (int t = 0; t < TT; ++t) read_b(0, 0, t);
   decode(0, 0);
   int ring = 0;                                          // stage % kStages
   for (int n = 0; n < n_chunk; ++n) {
-    const int chunk1 = (n + 1) * S::KS + part;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const int stage = n * W + j, ring1 = ring + 1 < S::kStages ? ring + 1 : 0;
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
+        // the next words and coefficients, where they landed a stage ago: beside these products
+        const bool turn = (j + 1) % GS == 0;             // the next stage's word begins a group
+        if (kFour && j + 1 == W && f == 0) read_w(w_next);
+        if (GS > 1 && turn && f == 0) read_c();
+        if (GS > 1 && turn && f == 1) make_levels(levels_next, stage + 1);
         if (f == 3) {
-          // A wait of the compiler's for its loads is one for the requests behind them too, and ours for requests is one for its loads
-          // before them: what they bring is taken before the next requests, and they are issued right before these.
-          if (j + 1 == W) take_w();
-          if ((j + 1) % GS == 0) store_levels(stage + 1);
           wait_vm<(S::kStages - 2) * S::kDma>();
+          asm volatile("" ::: "memory");
+          if (!kFour) read_w(w_next);
+          if (!kFour || j + 1 == W) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+              for (int i = 0; i < K; ++i)
+#pragma unroll
+                for (int e = 0; e < kW; ++e) w_cur[r][i][e] = w_next[r][i][e];
+          }
+          if (GS == 1) {
+            read_c();
+            make_levels(levels_next, stage + 1);
+          }
+          if (turn) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) levels[r] = levels_next[r];
+          }
           __syncthreads();
-          if (j == (S::kAcc <= 64 ? W - 1 : W / 2 - 1)) load_w(S::kAcc <= 64 ? chunk1 + S::KS : chunk1);
-          if ((j + 1) % GS == 0) load_levels(stage + 1 + GS);
-          if ((j + 1) % GS == 0) read_levels(stage + 1);
+          // (before the stage's first requests, so that the next stage's wait is one for these; a chunk's words a stage behind its
+          // coefficients, so that the wavefront is held up by fewer requests at once)
+          if (!kFour || j == 0) request_w(kFour ? stage - j + W : stage + 2);
+          if (turn) request_c(stage + 1 + GS);
         }
         // the slot of the stage before is free behind its barrier
         if (f == 3) request(stage + S::kStages, ring, 0);
