@@ -30,19 +30,20 @@ struct NormArgs {
   int vec_x, vec_r, vec_s, vec_w, vec_y;                  // by 16 bytes (codes: by 8)
 };
 
+// eight consecutive values as they lie in memory, zeros behind the n-th
 template <typename T>
-__device__ __forceinline__ void norm_load8(const T* __restrict__ p, bool vec, int n, float (&v)[8]) {
-  if (vec && n >= 8) {
-    alignas(16) T raw[8];
+struct NormEight {
+  alignas(16) T raw[8];
+  __device__ __forceinline__ void load(const T* __restrict__ p, bool vec, int n) {
+    if (vec && n >= 8) {
 #pragma unroll
-    for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(raw)[q] = reinterpret_cast<const u32x4_t*>(p)[q];
+      for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<u32x4_t*>(raw)[q] = reinterpret_cast<const u32x4_t*>(p)[q];
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)raw[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? (float)p[e] : 0.f;
+      for (int e = 0; e < 8; ++e) raw[e] = e < n ? p[e] : (T)0.f;
+    }
   }
-}
+};
 template <typename T>
 __device__ __forceinline__ void norm_store8(T* __restrict__ p, bool vec, int n, const float (&v)[8]) {
   if (vec && n >= 8) {
@@ -58,47 +59,50 @@ __device__ __forceinline__ void norm_store8(T* __restrict__ p, bool vec, int n, 
   }
 }
 
-// T: X, weight, Y; R: residual and sum; NV: turns of a thread.  blockDim.x = threads of a row, blockDim.y rows (1 unless a row is one wavefront's).
+// T: X, weight, Y; R: residual and sum; NV: turns of a thread.  blockDim.x = threads of a row, a power of two or whole wavefronts; blockDim.y rows (1
+// where a row is more than a wavefront's).
 template <typename T, typename R, int NV, bool Q8>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
   const int tid = threadIdx.x, per = blockDim.x, waves = per >> 6;
   const int row = blockIdx.x * blockDim.y + threadIdx.y;
   __shared__ double part_sum[16];
-  __shared__ uint32_t part_most[16];
-  if (row >= a.n_tok) return;                             // whole wavefronts, and only where rows are wavefronts' own
+  __shared__ float part_most[16];
+  if (row >= a.n_tok) return;                             // whole rows, which no barrier or shuffle crosses
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
   const R* r = a.residual ? static_cast<const R*>(a.residual) + row * a.ldr : nullptr;
-  float v[NV][8], w[NV][8];
+  NormEight<T> w[NV];
+  float v[NV][8];
+  {
+    NormEight<T> in[NV];
+    NormEight<R> add[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int at = 8 * (j * per + tid);
-    norm_load8(x + at, a.vec_x, a.d - at, v[j]);
-  }
-  if (r) {
+    for (int j = 0; j < NV; ++j) in[j].load(x + 8 * (j * per + tid), a.vec_x, a.d - 8 * (j * per + tid));
+    if (r) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int at = 8 * (j * per + tid);
-      float add[8];
-      norm_load8(r + at, a.vec_r, a.d - at, add);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] += add[e];
+      for (int j = 0; j < NV; ++j) add[j].load(r + 8 * (j * per + tid), a.vec_r, a.d - 8 * (j * per + tid));
     }
-  }
+    if (a.weight) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int at = 8 * (j * per + tid);
-    if (a.weight) norm_load8(static_cast<const T*>(a.weight) + at, a.vec_w, a.d - at, w[j]);
-    else
+      for (int j = 0; j < NV; ++j)
+        w[j].load(static_cast<const T*>(a.weight) + 8 * (j * per + tid), a.vec_w, a.d - 8 * (j * per + tid));
+    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[j][e] = 1.f;
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[j].raw[e] = (T)1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] = r ? (float)in[j].raw[e] + (float)add[j].raw[e] : (float)in[j].raw[e];
   }
   double sum = 0.0;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)v[j][e], (double)v[j][e], sum);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  const int lanes = per < 64 ? per : 64;
+  for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if (waves > 1) {
     if ((tid & 63) == 0) part_sum[tid >> 6] = sum;
     __syncthreads();
@@ -109,79 +113,66 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
   if (a.sum) {
     R* s = static_cast<R*>(a.sum) + row * a.lds;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int at = 8 * (j * per + tid);
-      norm_store8(s + at, a.vec_s, a.d - at, v[j]);
-    }
+    for (int j = 0; j < NV; ++j) norm_store8(s + 8 * (j * per + tid), a.vec_s, a.d - 8 * (j * per + tid), v[j]);
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] *= inv_rms * (a.offset + w[j][e]);
+    for (int e = 0; e < 8; ++e) v[j][e] *= inv_rms * (a.offset + (float)w[j].raw[e]);
   if constexpr (!Q8) {
     T* y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int at = 8 * (j * per + tid);
-      norm_store8(y + at, a.vec_y, a.d - at, v[j]);
-    }
+    for (int j = 0; j < NV; ++j) norm_store8(y + 8 * (j * per + tid), a.vec_y, a.d - 8 * (j * per + tid), v[j]);
   } else {
-    // largest magnitudes as bits: a NaN is above an infinity, an infinity above every number
-    uint32_t most[NV];
+    // (values behind the row's end are zero, whatever the weight; a maximum leaves out what is no number: the sum has it)
+    float most[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      most[j] = 0;
+      most[j] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t b = 8 * (j * per + tid) + e < a.d ? __builtin_bit_cast(uint32_t, v[j][e]) & 0x7fffffffu : 0u;
-        most[j] = most[j] > b ? most[j] : b;
-      }
+      for (int e = 0; e < 8; ++e) most[j] = fmaxf(most[j], fabsf(v[j][e]));
     }
     if (a.group == 0) {
 #pragma unroll
-      for (int j = 1; j < NV; ++j) most[0] = most[0] > most[j] ? most[0] : most[j];
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const uint32_t b = __shfl_xor(most[0], o, 64);
-        most[0] = most[0] > b ? most[0] : b;
-      }
+      for (int j = 1; j < NV; ++j) most[0] = fmaxf(most[0], most[j]);
+      for (int o = lanes >> 1; o > 0; o >>= 1) most[0] = fmaxf(most[0], __shfl_xor(most[0], o, 64));
       if (waves > 1) {
         if ((tid & 63) == 0) part_most[tid >> 6] = most[0];
         __syncthreads();
-        for (int q = 0; q < waves; ++q) most[0] = most[0] > part_most[q] ? most[0] : part_most[q];
+        for (int q = 0; q < waves; ++q) most[0] = fmaxf(most[0], part_most[q]);
       }
 #pragma unroll
       for (int j = 1; j < NV; ++j) most[j] = most[0];
     } else {
-      for (int o = a.group / 16; o > 0; o >>= 1) {
+      for (int o = a.group / 16; o > 0; o >>= 1) {        // (a group is 4 to 32 lanes, and no more than a row's)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          const uint32_t b = __shfl_xor(most[j], o, 64);
-          most[j] = most[j] > b ? most[j] : b;
-        }
+        for (int j = 0; j < NV; ++j) most[j] = fmaxf(most[j], __shfl_xor(most[j], o, 64));
       }
     }
-    const int n_scale = a.group ? a.d / a.group : 1;
+    const int unit = a.group ? a.group : a.d, n_scale = a.group ? a.d / a.group : 1;
+    const bool fine = sum < (double)__builtin_inf();      // no NaN and no infinity in the row
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int at = 8 * (j * per + tid);
       if (at >= a.d) break;
-      const float scale = most[j] >= 0x7f800000u ? __builtin_nanf("")
-                                                 : fmaxf(__builtin_bit_cast(float, most[j]), kNormFloor) * (1.0f / 127.0f);
-      const int unit = a.group ? a.group : a.d;
+      const float scale = fine ? fmaxf(most[j], kNormFloor) * (1.0f / 127.0f) : __builtin_nanf("");
       if (at % unit == 0) a.scales[(long)row * n_scale + at / unit] = scale;
       const float inv = 1.f / scale;
-      int8_t* c = a.codes + row * a.ldc + at;
-      uint32_t out[2] = {0, 0};
+      // y / scale to the nearest whole number, ties to even, in one rounding: behind 1.5 2^23 it is the low byte (of a NaN: 0)
+      uint32_t c[8], out[2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)                         // (a NaN becomes the lower bound)
-        out[e / 4] |= (uint32_t)((int)fminf(fmaxf(rintf(v[j][e] * inv), -127.f), 127.f) & 255) << (8 * (e % 4));
+      for (int e = 0; e < 8; ++e) c[e] = __builtin_bit_cast(uint32_t, fmaf(v[j][e], inv, 0x1.8p23f));
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        out[q] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[4 * q + 3], c[4 * q + 2], 0x0c0c0400u),
+                                       __builtin_amdgcn_perm(c[4 * q + 1], c[4 * q], 0x0c0c0400u), 0x05040100u);
+      int8_t* p = a.codes + row * a.ldc + at;
       if (a.vec_y && a.d - at >= 8) {
-        *reinterpret_cast<u32x2_t*>(c) = u32x2_t{out[0], out[1]};
+        *reinterpret_cast<u32x2_t*>(p) = u32x2_t{out[0], out[1]};
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (at + e < a.d) c[e] = (int8_t)(out[e / 4] >> (8 * (e % 4)));
+          if (at + e < a.d) p[e] = (int8_t)c[e];
       }
     }
   }
@@ -190,18 +181,25 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
 template <typename T, typename R, int NV, bool Q8>
 static int norm_launch(const NormArgs& a, hipStream_t stream) {
   const int turns = bpdq_ceil_div(bpdq_ceil_div(a.d, 8), NV);
-  const int per = bpdq_ceil_div(turns, 64) * 64, rows = per == 64 ? 4 : 1;
+  int per = 64;
+  if (turns > 64) per = bpdq_ceil_div(turns, 64) * 64;
+  else
+    while (per > 4 && per / 2 >= turns && 4 * per >= a.group) per /= 2;      // (a group's lanes are a row's)
+  const int rows = per > 64 ? 1 : 256 / per;
   hipLaunchKernelGGL((norm_kernel<T, R, NV, Q8>), dim3(bpdq_ceil_div(a.n_tok, rows)), dim3(per, rows), 0, stream, a);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
 
+// Turns of a thread, measured (us; bf16, with a residual in bf16, back to back in a graph): few rows want threads, 16 x 3584 3.2 with one
+// turn, 3.8 with two, but 333 x 8192 6.4 and 5.5; many rows two, 4096 x 8192 + fp32 79 with one, 74 with two and with four; wide rows so many that a
+// CU holds more than two of them: 1023 x 18944 to codes 24 with four turns (640 threads), 19 with five (512), 21 with six, 32 with eight.
 template <typename T, typename R, bool Q8>
 static int norm_pick(const NormArgs& a, hipStream_t stream) {
   const int vecs = bpdq_ceil_div(a.d, 8);
-  if (vecs <= 1024) return norm_launch<T, R, 1, Q8>(a, stream);
+  if (vecs <= 512 && a.n_tok <= 512) return norm_launch<T, R, 1, Q8>(a, stream);
   if (vecs <= 2048) return norm_launch<T, R, 2, Q8>(a, stream);
-  if (vecs <= 4096) return norm_launch<T, R, 4, Q8>(a, stream);
+  if (vecs <= 5120) return norm_launch<T, R, 5, Q8>(a, stream);
   return norm_launch<T, R, 8, Q8>(a, stream);
 }
 

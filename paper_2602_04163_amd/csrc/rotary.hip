@@ -2,8 +2,7 @@
 //   (a, b) -> m (a cos - b sin, b cos + a sin),    pairs (i, i + rot / 2) or (2 i, 2 i + 1), i < rot / 2; channels from rot on pass.
 //
 // Angles are formed in fp64 as turns, p f / 2 pi, of which only the fraction counts: at position 10^6 an fp32 angle would be off by 0.06.  The
-// fraction, as fp32 good to 2^-25 of a turn, goes to sincospif.  A work-group makes the angles of its tokens once, in LDS, for all heads of Q and K;
-// a thread keeps those of its channels in registers while it goes through the heads.
+// fraction, as fp32 good to 2^-26 of a turn, goes to sincospif.  A work-group makes the angles of its tokens once, in LDS, for all heads of Q and K.
 //
 // What bounds it: bytes, and for few tokens the launch.
 #include "common.h"
@@ -30,11 +29,25 @@ struct RotaryArgs {
   float mscale, sign;
 };
 
-// VEC: units of 16 bytes (of pairs: of both their halves where these lie apart), else single pairs and channels.
-template <typename T, bool VEC>
+// E consecutive channels at once
+template <typename T, int E>
+struct RotaryUnit {
+  alignas(E * sizeof(T)) T v[E];
+};
+
+// a c + b s, with the same roundings whichever units a call takes: left to itself the compiler fuses the last one into the conversion to fp16 in
+// some of them.
+__device__ __forceinline__ float rotary_turn(float a, float c, float b, float s) {
+  float sum = fmaf(a, c, b * s);
+  asm("" : "+v"(sum));
+  return sum;
+}
+
+// E: channels of a unit (of pairs that lie apart: of both their halves); 1: single pairs and channels.
+template <typename T, int E>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   __shared__ float2 turn[kRotPer * kRotDimMost / 2];
-  constexpr int E = VEC ? 16 / (int)sizeof(T) : 1;        // channels of a unit
+  typedef RotaryUnit<T, E> Unit;
   const int tid = threadIdx.x, seq = blockIdx.y, pairs = a.rot / 2;
   const long p0 = a.pos[seq], first = a.tok_start[seq];
   long n = (long)a.tok_start[seq + 1] - first;
@@ -53,78 +66,80 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   }
   __syncthreads();
 
-  // units of a head: those of pairs, then those that pass
-  const int paired = a.half || !VEC ? pairs / E : a.rot / E, units = paired + (a.dim - a.rot) / E;
+  // units of a head: those of pairs, then those that pass; its (token, head)s come to the threads of a unit in turn
+  const bool apart = a.half || E == 1;                    // a unit has the first channels of its pairs, and the second ones elsewhere
+  const int paired = apart ? pairs / E : a.rot / E, units = paired + (a.dim - a.rot) / E;
   const int wide = units < kRotThreads ? units : kRotThreads;
   const int slot = tid / wide, slots = kRotThreads / wide, heads = a.n_q + a.n_kv;
   if (slot >= slots) return;
-  const int near = VEC ? 0 : a.half ? pairs : 1;          // single pairs: from the first channel to the second
-  for (int t = 0; t < toks; ++t) {
-    const long row = first + from + t;
-    for (int u = tid % wide; u < units; u += wide) {
-      const bool turned = u < paired;
-      const int ch = turned ? (VEC || a.half ? u * E : 2 * u) : a.rot + (u - paired) * E;      // the unit's first channel
-      constexpr int P = VEC ? E : 1;                      // pairs of a unit at most
-      float c[P], s[P];
-      if (turned) {
+  const int step_t = slots / heads, step_h = slots - step_t * heads;
+  const int near = a.half ? pairs : 1;                    // from the first channel of a pair to the second
+  for (int u = tid % wide; u < units; u += wide) {
+    const bool turned = u < paired;
+    const int ch = !turned ? a.rot + (u - paired) * E : E == 1 && !a.half ? 2 * u : u * E;      // the unit's first channel
+    int h = slot % heads;
+    for (int t = slot / heads; t < toks;) {
+      const bool is_q = h < a.n_q;
+      if (turned || (is_q ? a.copy_q : a.copy_k)) {
+        const long row = first + from + t;
+        const T* p = (is_q ? static_cast<const T*>(a.q) + row * a.ldq + h * a.dim
+                           : static_cast<const T*>(a.k) + row * a.ldk + (h - a.n_q) * a.dim) + ch;
+        T* to = (is_q ? static_cast<T*>(a.q_out) + row * a.ldqo + h * a.dim
+                      : static_cast<T*>(a.k_out) + row * a.ldko + (h - a.n_q) * a.dim) + ch;
+        Unit x = *reinterpret_cast<const Unit*>(p);
+        if (turned && apart) {
+          Unit y = *reinterpret_cast<const Unit*>(p + near);
+          const float2* angle = turn + t * pairs + u * E;
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const int pair = !VEC ? u : a.half ? ch + e : ch / 2 + e / 2;
-          c[e] = turn[t * pairs + pair].x;
-          s[e] = turn[t * pairs + pair].y;
-        }
-      }
-      for (int h = slot; h < heads; h += slots) {
-        const bool is_q = h < a.n_q;
-        const T* from_p = is_q ? static_cast<const T*>(a.q) + row * a.ldq + (long)h * a.dim
-                               : static_cast<const T*>(a.k) + row * a.ldk + (long)(h - a.n_q) * a.dim;
-        T* to = is_q ? static_cast<T*>(a.q_out) + row * a.ldqo + (long)h * a.dim
-                     : static_cast<T*>(a.k_out) + row * a.ldko + (long)(h - a.n_q) * a.dim;
-        if constexpr (VEC) {
-          alignas(16) T x[E], y[E];
-          if (!turned) {
-            if (is_q ? a.copy_q : a.copy_k)
-              *reinterpret_cast<u32x4_t*>(to + ch) = *reinterpret_cast<const u32x4_t*>(from_p + ch);
-          } else if (a.half) {
-            *reinterpret_cast<u32x4_t*>(x) = *reinterpret_cast<const u32x4_t*>(from_p + ch);
-            *reinterpret_cast<u32x4_t*>(y) = *reinterpret_cast<const u32x4_t*>(from_p + ch + pairs);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const float p = (float)x[e], q = (float)y[e];
-              x[e] = (T)(p * c[e] - q * s[e]);
-              y[e] = (T)(q * c[e] + p * s[e]);
-            }
-            *reinterpret_cast<u32x4_t*>(to + ch) = *reinterpret_cast<const u32x4_t*>(x);
-            *reinterpret_cast<u32x4_t*>(to + ch + pairs) = *reinterpret_cast<const u32x4_t*>(y);
-          } else {
-            *reinterpret_cast<u32x4_t*>(x) = *reinterpret_cast<const u32x4_t*>(from_p + ch);
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-              const float p = (float)x[e], q = (float)x[e + 1];
-              x[e] = (T)(p * c[e] - q * s[e]);
-              x[e + 1] = (T)(q * c[e] + p * s[e]);
-            }
-            *reinterpret_cast<u32x4_t*>(to + ch) = *reinterpret_cast<const u32x4_t*>(x);
+          for (int e = 0; e < E; ++e) {
+            const float c = angle[e].x, s = angle[e].y, one = (float)x.v[e], two = (float)y.v[e];
+            x.v[e] = (T)(rotary_turn(one, c, -two, s));
+            y.v[e] = (T)(rotary_turn(two, c, one, s));
           }
+          *reinterpret_cast<Unit*>(to + near) = y;
         } else if (turned) {
-          const float p = (float)from_p[ch], q = (float)from_p[ch + near];
-          to[ch] = (T)(p * c[0] - q * s[0]);
-          to[ch + near] = (T)(q * c[0] + p * s[0]);
-        } else if (is_q ? a.copy_q : a.copy_k) {
-          to[ch] = from_p[ch];
+          const float2* angle = turn + t * pairs + u * (E / 2);
+#pragma unroll
+          for (int e = 0; e + 1 < E; e += 2) {
+            const float c = angle[e / 2].x, s = angle[e / 2].y, one = (float)x.v[e], two = (float)x.v[e + 1];
+            x.v[e] = (T)(rotary_turn(one, c, -two, s));
+            x.v[e + 1] = (T)(rotary_turn(two, c, one, s));
+          }
         }
+        *reinterpret_cast<Unit*>(to) = x;
+      }
+      h += step_h;
+      t += step_t;
+      if (h >= heads) {
+        h -= heads;
+        ++t;
       }
     }
   }
 }
 
-template <typename T>
-static int rotary_launch(const RotaryArgs& a, int n_seq, bool vec, hipStream_t stream) {
-  const dim3 grid(bpdq_ceil_div(a.max_tok, a.per), n_seq);
-  if (vec) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(kRotThreads), 0, stream, a);
-  else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(kRotThreads), 0, stream, a);
+template <typename T, int E>
+static int rotary_as(const RotaryArgs& a, int n_seq, hipStream_t stream) {
+  hipLaunchKernelGGL((rotary_kernel<T, E>), dim3(bpdq_ceil_div(a.max_tok, a.per), n_seq), dim3(kRotThreads), 0, stream, a);
   BPDQ_LAUNCH_CHECK();
   return 0;
+}
+
+// Units of 16 bytes where pairs, heads, rows and addresses are whole ones, of two channels where they are whole twos, else single ones: 4000 bf16
+// tokens of 40 heads of 80, 20 of these turned: 30 us by single ones.
+template <typename T>
+static int rotary_launch(const RotaryArgs& a, int n_seq, hipStream_t stream) {
+  auto whole = [&](int e) {
+    auto rows = [&](const void* p, long ld, int heads) {
+      return heads == 0 || (reinterpret_cast<uintptr_t>(p) % (e * sizeof(T)) == 0 && ld % e == 0);
+    };
+    return a.dim % e == 0 && (a.half ? a.rot / 2 : a.rot) % e == 0 && rows(a.q, a.ldq, a.n_q) && rows(a.k, a.ldk, a.n_kv) &&
+           rows(a.q_out, a.ldqo, a.n_q) && rows(a.k_out, a.ldko, a.n_kv);
+  };
+  constexpr int kWhole = 16 / (int)sizeof(T);
+  if (whole(kWhole)) return rotary_as<T, kWhole>(a, n_seq, stream);
+  if (whole(2)) return rotary_as<T, 2>(a, n_seq, stream);
+  return rotary_as<T, 1>(a, n_seq, stream);
 }
 
 }  // namespace bpdq
@@ -220,14 +235,8 @@ extern "C" int bpdq_rotary(const double* freq, int rot, int layout, float mscale
   a.per = 4;
   if ((long)bpdq_ceil_div(a.max_tok, 4) * n_seq < 1024) a.per = 1;
   if ((long)bpdq_ceil_div(a.max_tok, a.per) * kRotThreads > 0xffffffffL) return -10;           // threads along the grid's x
-  const int e = 16 / (int)size;
-  auto whole = [&](const void* p, long ld, int heads) {
-    return heads == 0 || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % e == 0);
-  };
-  const bool vec = head_dim % e == 0 && (a.half ? rot / 2 : rot) % e == 0 && whole(Q, ldq, n_q) && whole(K, ldk, n_kv) &&
-                   whole(Q_out, ldqo, n_q) && whole(K_out, ldko, n_kv);
   hipStream_t stream = static_cast<hipStream_t>(stream_);
-  if (dtype == BPDQ_F32) return rotary_launch<float>(a, n_seq, vec, stream);
-  if (dtype == BPDQ_F16) return rotary_launch<_Float16>(a, n_seq, vec, stream);
-  return rotary_launch<__bf16>(a, n_seq, vec, stream);
+  if (dtype == BPDQ_F32) return rotary_launch<float>(a, n_seq, stream);
+  if (dtype == BPDQ_F16) return rotary_launch<_Float16>(a, n_seq, stream);
+  return rotary_launch<__bf16>(a, n_seq, stream);
 }
