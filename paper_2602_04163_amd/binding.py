@@ -7,6 +7,7 @@ no CPU fallback -- a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -469,6 +470,8 @@ def _rows(t, dtype, shape, name):
     is expanded to several does)."""
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise BpdqError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
+    if t.is_contiguous():
+        return math.prod(shape[1:])
     strides = t.stride()
     step = 1
     for axis in range(len(shape) - 1, 0, -1):
@@ -493,6 +496,11 @@ def _here(*tensors):
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise BpdqError(f"a tensor on GPU {t.get_device()}, and the current one is {here}")
+
+
+def _like(t):
+    """A new tensor of dense rows."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _scratch(nbytes, device):
@@ -589,8 +597,7 @@ def _norm(X, weight, residual, S):
             raise BpdqError(f"residual: expected {dtype} or float32")
         ldr = _rows(residual, wide, shape, "residual")
         if S is None:
-            S = torch.empty(shape, dtype=wide, device=X.device)
-            lds = d
+            S, lds = _like(residual), d
         else:
             lds = _rows(S, wide, shape, "S")
     elif S is not None:
@@ -604,8 +611,7 @@ def bpdq_rms_norm(X, weight=None, eps=1e-6, residual=None, S=None, offset=0.0, Y
     Y = S / sqrt(mean(S^2) + eps) * (offset + weight) in X's.  S may be the residual, Y may be X."""
     args, S = _norm(X, weight, residual, S)
     if Y is None:
-        Y = torch.empty(X.shape, dtype=X.dtype, device=X.device)
-        ldy = X.shape[1]
+        Y, ldy = _like(X), X.shape[1]
     else:
         ldy = _rows(Y, X.dtype, X.shape, "Y")
     _here(X, weight, residual, S, Y)
@@ -666,7 +672,7 @@ def bpdq_rotary(freq, pos, tok_start, Q, K=None, max_tok=None, layout="half", ms
     n_tok, n_q, dim = Q.shape
     ldq, ldqo = _rows(Q, dtype, Q.shape, "Q"), n_q * dim
     if Q_out is None:
-        Q_out = torch.empty(Q.shape, dtype=dtype, device=Q.device)
+        Q_out = _like(Q)
     else:
         ldqo = _rows(Q_out, dtype, Q.shape, "Q_out")
     n_kv = ldk = ldko = 0
@@ -677,7 +683,7 @@ def bpdq_rotary(freq, pos, tok_start, Q, K=None, max_tok=None, layout="half", ms
         n_kv = K.shape[1]
         ldk, ldko = _rows(K, dtype, K.shape, "K"), n_kv * dim
         if K_out is None:
-            K_out = torch.empty(K.shape, dtype=dtype, device=K.device)
+            K_out = _like(K)
         else:
             ldko = _rows(K_out, dtype, K.shape, "K_out")
         k, k_out = K.data_ptr(), K_out.data_ptr()

@@ -40,19 +40,27 @@ __device__ __forceinline__ uint32_t sample_key(float x) {
   const uint32_t k = b >> 31 ? ~b : b | 0x80000000u;
   return x > -__builtin_inff() ? k : 0u;
 }
-// key and index as one number: larger values first, of equal ones the lower index
-__device__ __forceinline__ u64_t sample_place(uint32_t key, int i) { return (u64_t)key << 20 | (u64_t)(kSampleVocabMost - 1 - i); }
-__device__ __forceinline__ int sample_index(u64_t place) { return kSampleVocabMost - 1 - (int)(place & (kSampleVocabMost - 1)); }
-__device__ __forceinline__ uint32_t sample_key_of(u64_t place) { return (uint32_t)(place >> 20); }
 __device__ __forceinline__ float sample_value(uint32_t key) {
   return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key);
 }
+// Key and index as one number: larger values first, of equal ones the lower index.  A key goes without the bits that all values of the logits' type
+// share, so that equal values lie side by side, and bins over a range of places tell their indices apart.
+template <typename T>
+struct SamplePlace {
+  static constexpr int kDrop = __is_same(T, float) ? 0 : __is_same(T, _Float16) ? 13 : 16, kBits = 52 - kDrop;
+  static __device__ __forceinline__ u64_t of(uint32_t key, int i) { return (u64_t)(key >> kDrop) << 20 | (u64_t)(kSampleVocabMost - 1 - i); }
+  static __device__ __forceinline__ int index(u64_t place) { return kSampleVocabMost - 1 - (int)(place & (kSampleVocabMost - 1)); }
+  static __device__ __forceinline__ float value(u64_t place) {
+    const uint32_t key = (uint32_t)(place >> 20) << kDrop;
+    return sample_value(key >> 31 ? key : key | ((1u << kDrop) - 1));
+  }
+};
 
-// exp((x - M) / T) 2^43, rounded: 2^z by whole powers and the exponential's series for |fraction| <= 1/2 up to degree 11 (6e-15).  per: log2(e) / T.
-__device__ __forceinline__ unsigned long long sample_weight(float x, float most, double per) {
-  if (x == most) return 1ull << 43;
-  const double z = ((double)x - (double)most) * per;
-  if (!(z >= -45.0)) return 0;                            // (infinities apart make no number)
+// exp((x - M) / T) 2^43, rounded: 2^z by whole powers and the exponential's series for |fraction| <= 1/2 up to degree 11 (6e-15), without
+// branches.  per: log2(e) / T.
+__device__ __forceinline__ u64_t sample_weight(float x, float most, double per) {
+  // (a difference of infinities is no number, and goes the way of what is too small to count)
+  const double z = fmax(((double)x - (double)most) * per, -64.0);
   const double n = rint(z), f = (z - n) * 0.69314718055994530942;
   double e = 1.0 / 39916800.0;
   e = fma(e, f, 1.0 / 3628800.0);
@@ -67,7 +75,8 @@ __device__ __forceinline__ unsigned long long sample_weight(float x, float most,
   e = fma(e, f, 1.0);
   e = fma(e, f, 1.0);
   // the fraction's bits of a double in [2^52, 2^53) are its whole part
-  return __builtin_bit_cast(unsigned long long, ldexp(e, 43 + (int)n) + 0x1p52) & ((1ull << 52) - 1);
+  const u64_t w = __builtin_bit_cast(u64_t, ldexp(e, 43 + (int)n) + 0x1p52) & ((1ull << 52) - 1);
+  return x == most ? 1ull << 43 : w;
 }
 
 // part * total, up or down to a whole number, exactly; part in [0, 1]
@@ -105,40 +114,39 @@ __device__ __forceinline__ u64_t sample_lane(u64_t v, int lane) {
   return (u64_t)hi << 32 | lo;
 }
 
-// Sums and maxima over a work-group, and over the threads up to each one: one barrier each.  (Partial results lie in two places in turn: who
-// writes the first again has passed the barrier of the second, which all reach behind their reading of the first.)
+// Sums and maxima over a work-group, and over the threads up to each one: one barrier each, behind which every wavefront scans the
+// wavefronts' results by itself.  (These lie in two places in turn: who writes the first again has passed the barrier of the second, which all reach
+// behind their reading of the first.)
 template <int kThreads>
 struct SampleGroup {
   static constexpr int kWaves = kThreads / 64;
+  static_assert(kWaves >= 4 && kWaves <= 16, "a row of lanes");
   u64_t (&part)[2][kWaves];
   int turn = 0;
   __device__ __forceinline__ explicit SampleGroup(u64_t (&p)[2][kWaves]) : part(p) {}
 
+  // v: scanned over the wavefront.  Returns the scan over the wavefronts, lane w up to wavefront w.
   template <bool MAX>
-  __device__ __forceinline__ u64_t all(u64_t v) {
-    v = sample_wave_scan<MAX>(v);
+  __device__ __forceinline__ u64_t waves(u64_t v) {
+    auto join = [](u64_t a, u64_t b) { return MAX ? (a > b ? a : b) : a + b; };
     turn ^= 1;
     if ((threadIdx.x & 63) == 63) part[turn][threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) v = MAX ? (v > part[turn][w] ? v : part[turn][w]) : v + part[turn][w];
-    return v;
+    u64_t p = part[turn][threadIdx.x & (kWaves - 1)];
+    p = join(p, sample_dpp<0x111, 0xf>(p));
+    p = join(p, sample_dpp<0x112, 0xf>(p));
+    if (kWaves > 4) p = join(p, sample_dpp<0x114, 0xf>(p));
+    if (kWaves > 8) p = join(p, sample_dpp<0x118, 0xf>(p));
+    return p;
   }
-  __device__ __forceinline__ u64_t sum(u64_t v) { return all<false>(v); }
-  __device__ __forceinline__ u64_t max(u64_t v) { return all<true>(v); }
+  __device__ __forceinline__ u64_t sum(u64_t v) { return sample_lane(waves<false>(sample_wave_scan<false>(v)), kWaves - 1); }
+  __device__ __forceinline__ u64_t max(u64_t v) { return sample_lane(waves<true>(sample_wave_scan<true>(v)), kWaves - 1); }
   __device__ __forceinline__ u64_t scan(u64_t v, u64_t& total) {
     v = sample_wave_scan<false>(v);
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 63) part[turn][threadIdx.x >> 6] = v;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w == (int)(threadIdx.x >> 6)) v += total;
-      total += part[turn][w];
-    }
-    return v;
+    const u64_t p = waves<false>(v);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    total = sample_lane(p, kWaves - 1);
+    return wave > 0 ? v + sample_lane(p, wave - 1) : v;
   }
 };
 
@@ -165,14 +173,17 @@ struct SampleEight {
       for (int e = 0; e < 8; ++e) raw[e] = at + e >= 0 && at + e < n_vocab ? x[at + e] : (T)(-__builtin_inff());
     }
   }
-  // f(value, index) of what is there
+  // f(value, index) of what is there, or of all, minus infinity what is not
   template <typename F>
   __device__ __forceinline__ void each(int at, F f) const {
+    all(at, [&](float v, int i) {
+      if (v > -__builtin_inff()) f(v, i);
+    });
+  }
+  template <typename F>
+  __device__ __forceinline__ void all(int at, F f) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float v = (float)raw[e] + 0.f;                // (minus zero is zero)
-      if (v > -__builtin_inff()) f(v, at + e);
-    }
+    for (int e = 0; e < 8; ++e) f(fmaxf((float)raw[e] + 0.f, -__builtin_inff()), at + e);     // (minus zero is zero, and what is no number goes)
   }
 };
 
@@ -193,6 +204,7 @@ constexpr int kSampleTurn = kSampleChunkThreads * 8;      // values of a work-gr
 constexpr int kSampleChunks = 256;                        // of a row, at most
 constexpr int kSampleSteps = 3072;                        // 12 octaves of 256, from 2^-5 below the largest value to 2^7
 constexpr int kSampleList = 2048;
+constexpr int kSampleRanked = 128;                        // up to here every entry is compared with every other
 
 static int sample_chunks(int n_vocab, int turns) { return bpdq_ceil_div(n_vocab + 7, turns * kSampleTurn); }        // (with the skew)
 static int sample_turns(int n_tok, int n_vocab) {         // of a chunk
@@ -242,11 +254,12 @@ struct SampleAsk {
   u64_t least;                                            // the least weight that min-p leaves
   bool draw;                                              // not: the largest value is the answer
 };
+template <typename T>
 __device__ __forceinline__ SampleAsk sample_ask(const SampleArgs& a, int row, u64_t top) {
   SampleAsk ask;
   const float t = a.temperature ? a.temperature[row] : 1.f;
   ask.draw = top != 0 && t > 0.f;
-  ask.most = sample_value(sample_key_of(top));
+  ask.most = SamplePlace<T>::value(top);
   ask.per = 1.4426950408889634074 / (double)t;
   const int k = a.top_k ? a.top_k[row] : 0;
   ask.k = k > 0 && k < a.n_vocab ? k : 0;
@@ -276,14 +289,22 @@ struct SampleChunk {
     eight.load(x, first, n_vocab);
   }
   template <typename F>
-  __device__ __forceinline__ void each(F f) {
+  __device__ __forceinline__ void eights(F f) {
     for (int turn = 0; turn < turns; ++turn) {
       const int at = first + turn * kSampleTurn;
       SampleEight<T> next;
       if (turn + 1 < turns) next.load(x, at + kSampleTurn, n_vocab);
-      eight.each(at, f);
+      f(eight, at);
       eight = next;
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {             // f(value, index) of what is there
+    eights([&](const SampleEight<T>& v, int at) { v.each(at, f); });
+  }
+  template <typename F>
+  __device__ __forceinline__ void all(F f) {              // of all, minus infinity what is not
+    eights([&](const SampleEight<T>& v, int at) { v.all(at, f); });
   }
 };
 
@@ -306,10 +327,13 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleA
     if (chunk == 0 && threadIdx.x == 0) w.count[row] = 0;
   }
   u64_t top = 0;
-  values.each([&](float v, int i) {
-    const u64_t place = sample_place(sample_key(v), i);
-    top = top > place ? top : place;
+  float most = -__builtin_inff();
+  int at = 0;
+  values.all([&](float v, int i) {                        // (indices rise: the first of equal ones stays)
+    at = v > most ? i : at;
+    most = fmaxf(most, v);
   });
+  if (most > -__builtin_inff()) top = SamplePlace<T>::of(sample_key(most), at);
   top = group.max(top);
   if (threadIdx.x == 0) w.top[blockIdx.x] = top;
 }
@@ -323,12 +347,23 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(Sample
   if (!(a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.n_vocab) && !(a.top_p && a.top_p[row] < 1.f)) return;   // uniform: nothing to bound
   SampleChunk<T> values(a, w, row, chunk);
   for (int i = threadIdx.x; i < kSampleSteps; i += kSampleChunkThreads) hist[i] = 0;
-  const SampleAsk ask = sample_ask(a, row, sample_row_top(w, row, group));      // (its barrier is the histogram's too)
+  const SampleAsk ask = sample_ask<T>(a, row, sample_row_top(w, row, group));      // (its barrier is the histogram's too)
   if (!ask.draw) return;                                  // uniform
-  values.each([&](float v, int) {
-    const u64_t add = ask.k ? 1 : sample_weight(v, ask.most, ask.per);
-    if (add) atomicAdd(&hist[sample_step(v, ask.most)], add);
-  });
+  if (ask.k) {                                            // uniform
+    values.each([&](float v, int) { atomicAdd(&hist[sample_step(v, ask.most)], 1ull); });
+  } else {
+    values.eights([&](const SampleEight<T>& v, int at) {
+      u64_t add[8];
+      int step[8];
+      v.all(at, [&](float x, int i) {
+        add[i - at] = sample_weight(x, ask.most, ask.per);
+        step[i - at] = sample_step(x, ask.most);
+      });
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (add[e]) atomicAdd(&hist[step[e]], add[e]);
+    });
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < kSampleSteps; i += kSampleChunkThreads)
     if (hist[i]) atomicAdd(&w.hist[(long)row * kSampleSteps + i], hist[i]);
@@ -377,7 +412,7 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
   SampleChunk<T> values(a, w, row, chunk);
   if (threadIdx.x == 0) count = 0;
   const u64_t top = sample_row_top(w, row, group);
-  const SampleAsk ask = sample_ask(a, row, top);
+  const SampleAsk ask = sample_ask<T>(a, row, top);
   SampleBorder border = {top, 0, 0, kSampleSteps};
   if (ask.draw && (ask.k || ask.p < 1.f)) border = sample_border(w, ask, row, top, group, found);       // uniform
   if (chunk == 0 && threadIdx.x == 0) w.border[row] = border;
@@ -385,19 +420,24 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
   const int bin = (int)border.bin;
   const bool all = ask.k && ask.p < 1.f;                  // the whole top-k goes to the list
   u64_t sum = 0;
-  values.each([&](float v, int i) {
-    if (bin < kSampleSteps) {                             // uniform
+  auto add = [&](float v) {
+    const u64_t one = sample_weight(v, ask.most, ask.per);
+    sum += one >= ask.least ? one : 0;
+  };
+  if (bin == kSampleSteps) {                              // uniform
+    values.all([&](float v, int) { add(v); });
+  } else {
+    values.each([&](float v, int i) {
       const int step = sample_step(v, ask.most);
       if (step > bin) return;
       if (all || step == bin) {
         const int at = atomicAdd(&count, 1);
-        if (at < kSampleList) list[at] = sample_place(sample_key(v), i);
+        if (at < kSampleList) list[at] = SamplePlace<T>::of(sample_key(v), i);
         return;
       }
-    }
-    const u64_t one = sample_weight(v, ask.most, ask.per);
-    if (one >= ask.least) sum += one;
-  });
+      add(v);
+    });
+  }
   sum = group.sum(sum);
   if (threadIdx.x == 0) {
     w.sum[blockIdx.x] = sum;
@@ -415,7 +455,9 @@ typedef SampleGroup<kSampleThreads> SampleRowGroup;
 struct SampleShared {
   u64_t hist[kSampleBins];
   u64_t part[2][kSampleThreads / 64];
-  u64_t before, value, cut;
+  u64_t place[kSampleRanked], weight[kSampleRanked], above[kSampleRanked];       // of a list
+  int rank[kSampleRanked];
+  u64_t before, value;
   int bin;
 };
 static_assert(kSampleBins == kSampleThreads, "a thread to a bin");
@@ -463,10 +505,10 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const SampleAsk&
     u64_t prefix = 0;
     constexpr int kBits = 10;
     static_assert(kSampleBins == 1 << kBits, "digits");
-    for (int shift = 5 * kBits; shift >= 0; shift -= kBits) {       // 52 bits of a place
+    for (int shift = (SamplePlace<T>::kBits - 1) / kBits * kBits; shift >= 0; shift -= kBits) {
       sample_clear(sh);
       each([&](uint32_t key, int i) {
-        const u64_t place = sample_place(key, i);
+        const u64_t place = SamplePlace<T>::of(key, i);
         if (place >= cut && place >> (shift + kBits) == prefix) atomicAdd(&sh.hist[place >> shift & (kSampleBins - 1)], amount(key));
       });
       sample_find(sh, group, true, target);
@@ -481,7 +523,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const SampleAsk&
   if (ask.p < 1.f) {
     u64_t total = 0;
     each([&](uint32_t key, int i) {
-      if (sample_place(key, i) >= cut) total += weight(key);
+      if (SamplePlace<T>::of(key, i) >= cut) total += weight(key);
     });
     const u64_t target = sample_share(ask.p, group.sum(total), true);
     cut = select(target > 0 ? target : 1, weight);
@@ -493,7 +535,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const SampleAsk&
     sample_clear(sh);
     u64_t sum = 0;
     each([&](uint32_t key, int i) {
-      if (sample_place(key, i) < cut || (step == 1 && i / kSampleBins != block)) return;
+      if (SamplePlace<T>::of(key, i) < cut || (step == 1 && i / kSampleBins != block)) return;
       const u64_t w = weight(key);
       if (w < ask.least) return;
       atomicAdd(&sh.hist[step == 0 ? i / kSampleBins : i % kSampleBins], w);
@@ -520,10 +562,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
   constexpr int kEach = kSampleList / kSampleThreads;
   const int tid = threadIdx.x, row = blockIdx.x;
   const SampleBorder border = w.border[row];
-  const SampleAsk ask = sample_ask(a, row, border.top);
+  const SampleAsk ask = sample_ask<T>(a, row, border.top);
   if (!ask.draw) {                                        // uniform: nothing is there, or the largest is asked for
     if (tid == 0) {
-      a.token[row] = border.top ? sample_index(border.top) : -1;
+      a.token[row] = border.top ? SamplePlace<T>::index(border.top) : -1;
       if (a.prob) a.prob[row] = border.top ? 1.f : 0.f;
     }
     return;
@@ -546,29 +588,46 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
     for (int q = 0; q < kEach; ++q) {
       const int i = tid + q * kSampleThreads;
       place[q] = i < n ? w.list[(long)row * kSampleList + i] : 0;
-      weight[q] = i < n ? sample_weight(sample_value(sample_key_of(place[q])), ask.most, ask.per) : 0;
+      weight[q] = i < n ? sample_weight(SamplePlace<T>::value(place[q]), ask.most, ask.per) : 0;
     }
-    if (n <= 64) {
-      // one wavefront: everyone's rank and the weight above
-      if (tid < 64) {
-        u64_t above = 0;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) {
-          const bool larger = sample_lane(place[0], j) > place[0];
-          rank += larger;
-          above += larger ? sample_lane(weight[0], j) : 0;
-        }
-        bool in = tid < n;
-        if (both) {                                       // top-p of the exact top-k
-          in = in && rank < ask.k;
-          const u64_t total = sample_lane(sample_wave_scan<false>(in ? weight[0] : 0), 63), target = sample_share(ask.p, total, true);
-          in = in && above < (target > 0 ? target : 1);
-        } else {
-          in = in && border.before + (ask.k ? (u64_t)rank : above) < border.target;
-        }
-        const u64_t last = sample_lane(sample_wave_scan<true>(in ? ~place[0] : 0), 63);
-        if (tid == 0) sh.cut = ~last;
+    if (n <= kSampleRanked) {
+      // everyone's rank and the weight above, the list dealt to the threads of an entry
+      const int wide = n <= 64 ? 64 : kSampleRanked, parts = kSampleThreads / wide;
+      if (tid < wide) {
+        sh.place[tid] = place[0];
+        sh.weight[tid] = weight[0];
+        sh.above[tid] = 0;
+        sh.rank[tid] = 0;
       }
+      __syncthreads();
+      const int me = tid & (wide - 1), share = bpdq_ceil_div(n, parts), end = (tid / wide + 1) * share;
+      const u64_t mine = sh.place[me];
+      u64_t above = 0;
+      int rank = 0;
+#pragma unroll 4
+      for (int j = end - share; j < (end < n ? end : n); ++j) {
+        const bool larger = sh.place[j] > mine;
+        rank += larger;
+        above += larger ? sh.weight[j] : 0;
+      }
+      if (rank) {
+        atomicAdd(&sh.rank[me], rank);
+        atomicAdd(&sh.above[me], above);
+      }
+      __syncthreads();
+      bool in = tid < n;
+      if (in) {
+        rank = sh.rank[tid];
+        above = sh.above[tid];
+      }
+      if (both) {                                         // top-p of the exact top-k
+        in = in && rank < ask.k;
+        const u64_t target = sample_share(ask.p, group.sum(in ? weight[0] : 0), true);
+        in = in && above < (target > 0 ? target : 1);
+      } else {
+        in = in && border.before + (ask.k ? (u64_t)rank : above) < border.target;
+      }
+      cut = ~group.max(in ? ~place[0] : 0);
     } else {
       // The place at which the running sum over the list, from the largest on, reaches `target`: 1024 bins over what is left of its range at
       // a time, until a bin holds one.
@@ -598,7 +657,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
           int in = 0;
 #pragma unroll
           for (int q = 0; q < kEach; ++q) in += place[q] >= lo && place[q] <= hi;
-          if (shift == 0 || (__syncthreads_count(in > 0) <= 1 && !__syncthreads_or(in > 1))) return lo;
+          if (shift == 0 || group.sum(in) <= 1) return lo;
         }
       };
       if (both) {
@@ -614,14 +673,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
       }
       __syncthreads();
       sh.hist[tid] = mine;
-      if (tid == 0) sh.cut = cut;
+      __syncthreads();
     }
-    __syncthreads();
-    cut = sh.cut;
 #pragma unroll
     for (int q = 0; q < kEach; ++q)
       if (place[q] >= cut && weight[q] >= ask.least)      // (an empty place has no weight)
-        atomicAdd(&sh.hist[(sample_index(place[q]) + skew) / span], weight[q]);
+        atomicAdd(&sh.hist[(SamplePlace<T>::index(place[q]) + skew) / span], weight[q]);
   }
   __syncthreads();
   // the chunk, and in it a thread's consecutive values
@@ -638,7 +695,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
   auto one = [&](int i) -> u64_t {
     if (i < 0 || i >= a.n_vocab) return 0;
     const uint32_t key = sample_key((float)x[i]);
-    if (key == 0 || sample_place(key, i) < cut) return 0;
+    if (key == 0 || SamplePlace<T>::of(key, i) < cut) return 0;
     const u64_t v = sample_weight(sample_value(key), ask.most, ask.per);
     return v >= ask.least ? v : 0;
   };

@@ -16,6 +16,7 @@ def stand_in(monkeypatch):
     monkeypatch.setattr(bq, "_lib", Library())
     monkeypatch.setattr(bq, "_here", lambda *tensors: None)
     monkeypatch.setattr(torch, "empty", lambda *a, device=None, empty=torch.empty, **kw: gpu(empty(*a, **kw)))
+    monkeypatch.setattr(bq, "_like", lambda t: gpu(torch.zeros(t.shape, dtype=t.dtype)))
 
 
 def of(*shape, dtype=HALF):
