@@ -200,6 +200,7 @@ struct SampleEight {
 // rows of equal values, a very large top_k before top-p) leaves the row to one work-group, which selects by radix over the row itself.
 
 constexpr int kSampleChunkThreads = 256;
+constexpr int kSampleChunkWaves = kSampleChunkThreads / 64;
 constexpr int kSampleTurn = kSampleChunkThreads * 8;      // values of a work-group's turn
 constexpr int kSampleChunks = 256;                        // of a row, at most
 constexpr int kSampleSteps = 3072;                        // 12 octaves of 256, from 2^-5 below the largest value to 2^7
@@ -218,13 +219,15 @@ static int sample_turns(int n_tok, int n_vocab) {         // of a chunk
 struct SampleBorder {
   u64_t top;                                              // its largest value
   u64_t target, before;                                   // counts or weights: what is to be reached, and what lies above the bin
-  u64_t bin;                                              // of the histogram; kSampleSteps: nothing is bounded
+  int bin;                                                // of the histogram; kSampleSteps: nothing is bounded
+  int all;                                                // the list has everything down to the bin, not only what is in it
 };
 
 struct SampleWork {
   u64_t* top;                                             // [row][chunk]
   u64_t* sum;                                             // [row][chunk]
   u64_t* hist;                                            // [row][kSampleSteps]
+  float* high;                                            // [row][chunk][turn][wavefront] largest values
   u64_t* list;                                            // [row][kSampleList]
   SampleBorder* border;                                   // [row]
   int* count;                                             // [row] of the list; above kSampleList: it did not fit
@@ -241,6 +244,7 @@ static size_t sample_work(SampleWork& w, void* ws, int n_tok, int n_vocab) {
   w.hist = arena.take<u64_t>(n * kSampleSteps);
   w.list = arena.take<u64_t>(n * kSampleList);
   w.border = arena.take<SampleBorder>(n);
+  w.high = arena.take<float>(n * w.chunks * w.turns * kSampleChunkWaves);
   w.count = arena.take<int>(n);
   return arena.off;
 }
@@ -316,39 +320,102 @@ __device__ __forceinline__ u64_t sample_row_top(const SampleWork& w, int row, Sa
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleArgs a, SampleWork w, bool clear) {
-  __shared__ u64_t part[2][kSampleChunkThreads / 64];
+__global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleArgs a, SampleWork w, bool bounded) {
+  __shared__ u64_t part[2][kSampleChunkWaves];
   SampleChunkGroup group(part);
   const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks;
   SampleChunk<T> values(a, w, row, chunk);
-  if (clear) {
+  if (bounded) {
     for (int i = chunk * kSampleChunkThreads + threadIdx.x; i < kSampleSteps; i += w.chunks * kSampleChunkThreads)
       w.hist[(long)row * kSampleSteps + i] = 0;
     if (chunk == 0 && threadIdx.x == 0) w.count[row] = 0;
   }
-  u64_t top = 0;
   float most = -__builtin_inff();
   int at = 0;
-  values.all([&](float v, int i) {                        // (indices rise: the first of equal ones stays)
-    at = v > most ? i : at;
-    most = fmaxf(most, v);
+  float* high = w.high + (long)blockIdx.x * w.turns * kSampleChunkWaves + (threadIdx.x >> 6);
+  values.eights([&](const SampleEight<T>& v, int first) {
+    float here = -__builtin_inff();
+    v.all(first, [&](float x, int i) {                    // (indices rise: the first of equal ones stays)
+      at = x > most ? i : at;
+      most = fmaxf(most, x);
+      here = fmaxf(here, x);
+    });
+    if (bounded) {
+      const u64_t key = sample_lane(sample_wave_scan<true>(sample_key(here)), 63);
+      if ((threadIdx.x & 63) == 0) *high = key ? sample_value((uint32_t)key) : -__builtin_inff();
+      high += kSampleChunkWaves;
+    }
   });
-  if (most > -__builtin_inff()) top = SamplePlace<T>::of(sample_key(most), at);
-  top = group.max(top);
+  const u64_t top = group.max(most > -__builtin_inff() ? SamplePlace<T>::of(sample_key(most), at) : 0);
   if (threadIdx.x == 0) w.top[blockIdx.x] = top;
 }
+
+// where a histogram reaches its target, by a whole work-group: hist(step) its bins; found: two words of LDS
+template <typename F>
+__device__ __forceinline__ SampleBorder sample_border(const SampleAsk& ask, u64_t top, SampleChunkGroup& group, u64_t* found, F bin_of) {
+  constexpr int kEach = kSampleSteps / kSampleChunkThreads;
+  static_assert(kEach * kSampleChunkThreads == kSampleSteps, "whole shares");
+  u64_t hist[kEach], mine = 0, total;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) hist[e] = bin_of(threadIdx.x * kEach + e);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) mine += hist[e];
+  if (threadIdx.x == 0) found[0] = kSampleSteps;
+  const u64_t run = group.scan(mine, total);
+  SampleBorder s;
+  s.top = top;
+  s.all = ask.k && ask.p < 1.f;
+  s.target = ask.k ? (u64_t)ask.k : sample_share(ask.p, total, true);
+  if (s.target == 0) s.target = 1;
+  u64_t before = run - mine;
+  if (run >= s.target && before < s.target) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      if (before < s.target && before + hist[e] >= s.target) {
+        found[0] = threadIdx.x * kEach + e;
+        found[1] = before;
+      }
+      before += hist[e];
+    }
+  }
+  __syncthreads();
+  s.bin = (int)found[0];
+  s.before = s.bin < kSampleSteps ? found[1] : 0;
+  return s;
+}
+
+// Where a row asks for few of its largest values, there are as many above the k-th largest of its turns' largest ones: these are counted in place of
+// all values, by the row's first work-group, and the list takes what is above.  (If half of the turns hold one of N values, N is 0.69 of
+// the turns, 1.4 times their half.)
+__device__ __forceinline__ bool sample_few(const SampleWork& w, int k) { return 2L * k <= w.chunks * w.turns * kSampleChunkWaves; }
 
 template <typename T>
 __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(SampleArgs a, SampleWork w) {
   __shared__ u64_t hist[kSampleSteps];
-  __shared__ u64_t part[2][kSampleChunkThreads / 64];
+  __shared__ u64_t part[2][kSampleChunkWaves], found[2];
   SampleChunkGroup group(part);
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks;
-  if (!(a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.n_vocab) && !(a.top_p && a.top_p[row] < 1.f)) return;   // uniform: nothing to bound
+  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, highs = w.chunks * w.turns * kSampleChunkWaves;
+  const int k = a.top_k && a.top_k[row] > 0 && a.top_k[row] < a.n_vocab ? a.top_k[row] : 0;
+  if (k == 0 && !(a.top_p && a.top_p[row] < 1.f)) return;                                      // uniform: nothing to bound
+  const bool few = k > 0 && sample_few(w, k);
+  if (few && chunk > 0) return;                           // uniform
   SampleChunk<T> values(a, w, row, chunk);
   for (int i = threadIdx.x; i < kSampleSteps; i += kSampleChunkThreads) hist[i] = 0;
-  const SampleAsk ask = sample_ask<T>(a, row, sample_row_top(w, row, group));      // (its barrier is the histogram's too)
+  const u64_t top = sample_row_top(w, row, group);        // (its barrier is the histogram's too)
+  const SampleAsk ask = sample_ask<T>(a, row, top);
   if (!ask.draw) return;                                  // uniform
+  if (few) {
+    for (int i = threadIdx.x; i < highs; i += kSampleChunkThreads) {
+      const float v = w.high[(long)row * highs + i];
+      if (v > -__builtin_inff()) atomicAdd(&hist[sample_step(v, ask.most)], 1ull);
+    }
+    __syncthreads();
+    SampleBorder border = sample_border(ask, top, group, found, [&](int i) { return hist[i]; });
+    if (border.bin == kSampleSteps) border.bin = kSampleSteps - 1;       // fewer turns than that have values
+    border.all = 1;
+    if (threadIdx.x == 0) w.border[row] = border;
+    return;
+  }
   if (ask.k) {                                            // uniform
     values.each([&](float v, int) { atomicAdd(&hist[sample_step(v, ask.most)], 1ull); });
   } else {
@@ -369,42 +436,9 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(Sample
     if (hist[i]) atomicAdd(&w.hist[(long)row * kSampleSteps + i], hist[i]);
 }
 
-// where the histogram reaches its target, by a whole work-group; found: two words of LDS
-__device__ __forceinline__ SampleBorder sample_border(const SampleWork& w, const SampleAsk& ask, int row, u64_t top, SampleChunkGroup& group,
-                                                      u64_t* found) {
-  constexpr int kEach = kSampleSteps / kSampleChunkThreads;
-  static_assert(kEach * kSampleChunkThreads == kSampleSteps, "whole shares");
-  u64_t hist[kEach], mine = 0, total;
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) hist[e] = w.hist[(long)row * kSampleSteps + threadIdx.x * kEach + e];
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) mine += hist[e];
-  if (threadIdx.x == 0) found[0] = kSampleSteps;
-  const u64_t run = group.scan(mine, total);
-  SampleBorder s;
-  s.top = top;
-  s.target = ask.k ? (u64_t)ask.k : sample_share(ask.p, total, true);
-  if (s.target == 0) s.target = 1;
-  u64_t before = run - mine;
-  if (run >= s.target && before < s.target) {
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      if (before < s.target && before + hist[e] >= s.target) {
-        found[0] = threadIdx.x * kEach + e;
-        found[1] = before;
-      }
-      before += hist[e];
-    }
-  }
-  __syncthreads();
-  s.bin = found[0];
-  s.before = s.bin < kSampleSteps ? found[1] : 0;
-  return s;
-}
-
 template <typename T>
 __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(SampleArgs a, SampleWork w) {
-  __shared__ u64_t part[2][kSampleChunkThreads / 64], found[2];
+  __shared__ u64_t part[2][kSampleChunkWaves], found[2];
   __shared__ u64_t list[kSampleList];
   __shared__ int count, from;
   SampleChunkGroup group(part);
@@ -413,19 +447,46 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
   if (threadIdx.x == 0) count = 0;
   const u64_t top = sample_row_top(w, row, group);
   const SampleAsk ask = sample_ask<T>(a, row, top);
-  SampleBorder border = {top, 0, 0, kSampleSteps};
-  if (ask.draw && (ask.k || ask.p < 1.f)) border = sample_border(w, ask, row, top, group, found);       // uniform
-  if (chunk == 0 && threadIdx.x == 0) w.border[row] = border;
+  SampleBorder border = {top, 0, 0, kSampleSteps, 0};
+  if (ask.k && sample_few(w, ask.k) && ask.draw) {        // uniform
+    border = w.border[row];
+  } else {
+    if (ask.draw && (ask.k || ask.p < 1.f))
+      border = sample_border(ask, top, group, found, [&](int i) { return w.hist[(long)row * kSampleSteps + i]; });
+    if (chunk == 0 && threadIdx.x == 0) w.border[row] = border;
+  }
   if (!ask.draw) return;                                  // uniform
-  const int bin = (int)border.bin;
-  const bool all = ask.k && ask.p < 1.f;                  // the whole top-k goes to the list
+  const int bin = border.bin;
+  const bool all = border.all;
   u64_t sum = 0;
   auto add = [&](float v) {
     const u64_t one = sample_weight(v, ask.most, ask.per);
     sum += one >= ask.least ? one : 0;
   };
-  if (bin == kSampleSteps) {                              // uniform
+  if (bin == kSampleSteps && ask.least > 1) {             // uniform: few are likely
+    // (fp32 is off by less than 2^-10 of an exponent below 2^12; further down nothing reaches min-p)
+    const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = (float)ask.per;
+    values.all([&](float v, int) {
+      if (!((v - ask.most) * per < low)) add(v);
+    });
+  } else if (bin == kSampleSteps) {
     values.all([&](float v, int) { add(v); });
+  } else if (ask.k == 0) {
+    values.eights([&](const SampleEight<T>& v, int at) {
+      u64_t one[8];
+      int step[8];
+      v.all(at, [&](float x, int i) {
+        step[i - at] = x > -__builtin_inff() ? sample_step(x, ask.most) : kSampleSteps;
+        one[i - at] = sample_weight(x, ask.most, ask.per);
+      });
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += step[e] < bin && one[e] >= ask.least ? one[e] : 0;
+      v.all(at, [&](float x, int i) {
+        if (step[i - at] != bin) return;
+        const int to = atomicAdd(&count, 1);
+        if (to < kSampleList) list[to] = SamplePlace<T>::of(sample_key(x), i);
+      });
+    });
   } else {
     values.each([&](float v, int i) {
       const int step = sample_step(v, ask.most);
@@ -572,10 +633,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
   }
   const T* x = static_cast<const T*>(a.logits) + row * a.ld;
   const int skew = sample_skew(x), span = w.turns * kSampleTurn;
-  const bool both = ask.k && ask.p < 1.f;
   const int n = border.bin < kSampleSteps ? w.count[row] : 0;
   // (a top-k that keeps everything before a top-p has no histogram of weights)
-  if (n > kSampleList || (border.bin == kSampleSteps && both)) {       // uniform
+  if (n > kSampleList || (border.bin == kSampleSteps && ask.k && ask.p < 1.f)) {       // uniform
     sample_row<T>(a, ask, row, sh, group);
     return;
   }
@@ -620,10 +680,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
         rank = sh.rank[tid];
         above = sh.above[tid];
       }
-      if (both) {                                         // top-p of the exact top-k
+      if (border.all) {                                   // the exact top-k, and its top-p
         in = in && rank < ask.k;
-        const u64_t target = sample_share(ask.p, group.sum(in ? weight[0] : 0), true);
-        in = in && above < (target > 0 ? target : 1);
+        if (ask.p < 1.f) {
+          const u64_t target = sample_share(ask.p, group.sum(in ? weight[0] : 0), true);
+          in = in && above < (target > 0 ? target : 1);
+        }
       } else {
         in = in && border.before + (ask.k ? (u64_t)rank : above) < border.target;
       }
@@ -649,7 +711,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
           for (int q = 0; q < kEach; ++q)
             if (place[q] >= lo && place[q] <= hi) atomicAdd(&sh.hist[(place[q] - lo) >> shift], count ? 1ull : weight[q]);
           sample_find(sh, group, true, target);
-          if (sh.bin < 0) return lo;                      // (cannot be: the histogram counted these)
+          if (sh.bin < 0) return lo;                      // there are not so many
           target -= sh.before;
           lo += (u64_t)sh.bin << shift;
           const u64_t end = lo + ((1ull << shift) - 1);
@@ -660,14 +722,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_join_kernel(SampleArgs 
           if (shift == 0 || group.sum(in) <= 1) return lo;
         }
       };
-      if (both) {
+      if (border.all) {
         cut = select((u64_t)ask.k, 0, true);
-        u64_t total = 0;
+        if (ask.p < 1.f) {
+          u64_t total = 0;
 #pragma unroll
-        for (int q = 0; q < kEach; ++q)
-          if (place[q] >= cut) total += weight[q];
-        const u64_t target = sample_share(ask.p, group.sum(total), true);
-        cut = select(target > 0 ? target : 1, cut, false);
+          for (int q = 0; q < kEach; ++q)
+            if (place[q] >= cut) total += weight[q];
+          const u64_t target = sample_share(ask.p, group.sum(total), true);
+          cut = select(target > 0 ? target : 1, cut, false);
+        }
       } else {
         cut = select(border.target - border.before, 0, ask.k != 0);
       }
