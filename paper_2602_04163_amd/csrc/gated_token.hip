@@ -1,11 +1,69 @@
 // The gated product (linear.h) for one token: the look-ups of gemv.hip, gate and up row of a value by the same wavefront.
 //
-// What bounds it: the look-ups' vector instructions and LDS reads beside the memory, as there.  Against the few-token kernel of the matrix
-// instructions, which decodes weights that one token uses once.
+// What bounds it: the look-ups' vector instructions and LDS reads beside the memory, as there.  2 x 18944 x 3584 at 2 bits in groups of 128, one
+// bf16 token: 13.5 us (40 MB, 3.0 TB/s); the few-token kernel of the matrix instructions (linear.h) takes 26, since it decodes weights that one token
+// uses once.  Sums are of exact products in fp32, so a weight is not rounded to fp16 here.
 #include "gemv.h"
 #include "linear.h"
 
 namespace bpdq {
+
+// The 16 partial sums of four consecutive values of x, in table order, to t[0], t[64], ...
+__device__ __forceinline__ void gemv_table(float4 v, float* __restrict__ t) {
+  const float s01 = v.x + v.y, s23 = v.z + v.w;
+  const float e[16] = {0.f,  v.x,       v.y,       s01,       v.z, v.x + v.z, v.y + v.z, s01 + v.z,
+                       v.w,  v.x + v.w, v.y + v.w, s01 + v.w, s23, v.x + s23, v.y + s23, s01 + s23};
+#pragma unroll
+  for (int n = 0; n < 16; ++n) t[n * 64] = e[n];
+}
+
+// Sums over the lane's words of each row: C_0 S + sum_i C_i (look-ups), the table at LDS address 0.  (gemv.hip has these loops in its kernel: called
+// there, they are scheduled worse, 5000 x 8224 at 4 bits 16 -> 20 us, 18944 x 8320 at 2 bits 23 -> 35.)
+template <int K, int W, int NG, int ROWS, bool STRIDED, typename Item>
+__device__ __forceinline__ void gemv_rows(const Item& cur, const float* __restrict__ Sw, int n_word, int lane, float (&sum)[ROWS]) {
+#pragma unroll
+  for (int q = 0; q < ROWS; ++q) sum[q] = 0.f;
+  const unsigned base0 = 4u * lane, base1 = 4u * lane + 65536u;
+  typedef const __attribute__((address_space(3))) float lds_float;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    if (STRIDED && g > 0 && 64 * g >= n_word) break;       // uniform
+    float s = 0.f;
+#pragma unroll
+    for (int j = g * (W / NG); j < (g + 1) * (W / NG); ++j) s += Sw[j * 64 + lane];
+    const bool on = !STRIDED || 64 * g + lane < n_word;
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) {
+      float t = fmaf(cur.coef(q, 0, g), s, sum[q]);
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        float m = 0.f;                                     // one chain of eight adds per word
+#pragma unroll
+        for (int j = g * (W / NG); j < (g + 1) * (W / NG); ++j) {
+          float mj = 0.f;
+          const uint32_t w = cur.w[q][i][j];
+          const uint32_t ev = w & 0x0f0f0f0fu, od = (w >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+          for (int n = 0; n < 8; ++n) {
+            // address bytes: 0 = lane, 1 = the nibble, 2 and 3 = upper half of the table or not
+            const unsigned off = (unsigned)(n * W + j) * 4096u;
+            const unsigned a = __builtin_amdgcn_perm((n & 1) ? od : ev, off >= 65536u ? base1 : base0,
+                                                     0x03020000u | (unsigned)((4 + (n >> 1)) << 8));
+            mj += *reinterpret_cast<lds_float*>(a + (off & 65535u));
+          }
+          m += mj;
+        }
+        t = fmaf(cur.coef(q, i + 1, g), m, t);
+      }
+      // a word past the end adds nothing, whatever its coefficient (zero times an infinite one is not zero)
+      sum[q] = on ? t : sum[q];
+    }
+  }
+  if (!STRIDED && W * lane >= n_word) {
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q) sum[q] = 0.f;
+  }
+}
 
 // One chunk: d_in <= 2048 W.  ROWS = 2: an item is both rows; 1: an item is one of them, the gate's first.
 template <int K, int W, int NG, int ROWS, bool STRIDED>
@@ -73,8 +131,7 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
     if (f >= half) break;                                // uniform over the wavefront
     if (item + 1 < passes * kItems) fetch(item + 1, nxt);
     float v[ROWS];
-#pragma unroll
-    for (int q = 0; q < ROWS; ++q) v[q] = gemv_row<K, W, NG, STRIDED>(cur, q, Sw, nw, lane);
+    gemv_rows<K, W, NG, ROWS, STRIDED>(cur, Sw, nw, lane, v);
 #pragma unroll
     for (int q = 0; q < ROWS; ++q)
 #pragma unroll

@@ -97,52 +97,4 @@ __device__ __forceinline__ void gemv_fetch(const uint32_t* __restrict__ planes, 
   }
 }
 
-// The 16 partial sums of four consecutive values of x, in table order, to t[0], t[64], ...
-__device__ __forceinline__ void gemv_table(float4 v, float* __restrict__ t) {
-  const float s01 = v.x + v.y, s23 = v.z + v.w;
-  const float e[16] = {0.f,  v.x,       v.y,       s01,       v.z, v.x + v.z, v.y + v.z, s01 + v.z,
-                       v.w,  v.x + v.w, v.y + v.w, s01 + v.w, s23, v.x + s23, v.y + s23, s01 + s23};
-#pragma unroll
-  for (int n = 0; n < 16; ++n) t[n * 64] = e[n];
-}
-
-// sum over the lane's words of one row: C_0 S + sum_i C_i (look-ups), the table at LDS address 0
-template <int K, int W, int NG, bool STRIDED, typename Item>
-__device__ __forceinline__ float gemv_row(const Item& it, int q, const float* __restrict__ Sw, int n_word, int lane) {
-  const unsigned base0 = 4u * lane, base1 = 4u * lane + 65536u;
-  typedef const __attribute__((address_space(3))) float lds_float;
-  float sum = 0.f;
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    if (STRIDED && g > 0 && 64 * g >= n_word) break;       // uniform
-    float s = 0.f;
-#pragma unroll
-    for (int j = g * (W / NG); j < (g + 1) * (W / NG); ++j) s += Sw[j * 64 + lane];
-    float t = fmaf(it.coef(q, 0, g), s, sum);
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      float m = 0.f;                                       // one chain of eight adds per word
-#pragma unroll
-      for (int j = g * (W / NG); j < (g + 1) * (W / NG); ++j) {
-        float mj = 0.f;
-        const uint32_t w = it.w[q][i][j];
-        const uint32_t ev = w & 0x0f0f0f0fu, od = (w >> 4) & 0x0f0f0f0fu;
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-          // address bytes: 0 = lane, 1 = the nibble, 2 and 3 = upper half of the table or not
-          const unsigned off = (unsigned)(n * W + j) * 4096u;
-          const unsigned a = __builtin_amdgcn_perm((n & 1) ? od : ev, off >= 65536u ? base1 : base0,
-                                                   0x03020000u | (unsigned)((4 + (n >> 1)) << 8));
-          mj += *reinterpret_cast<lds_float*>(a + (off & 65535u));
-        }
-        m += mj;
-      }
-      t = fmaf(it.coef(q, i + 1, g), m, t);
-    }
-    // a word past the end adds nothing, whatever its coefficient (zero times an infinite one is not zero)
-    sum = !STRIDED || 64 * g + lane < n_word ? t : sum;
-  }
-  return !STRIDED && W * lane >= n_word ? 0.f : sum;
-}
-
 }  // namespace bpdq

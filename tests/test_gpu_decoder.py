@@ -604,3 +604,25 @@ def test_captured_and_replayed(dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+# ------------------------------------------------------------------ all of them together
+
+def test_the_example(dev):
+    """The decoder of the example, prompts of two sequences and tokens behind them: the tokens are those that the served logits ask for.  Logits:
+    every layer's attention is off by up to 4 % of its own size (the 8-bit cache: the attention's example), the other calls by roundings to
+    bfloat16 (2^-9 of a value each, some ten to a layer), and what a layer adds to the residual stream is not larger than the stream: below
+    4 % + 10 2^-9 = 6 % a layer, two layers, and the last norm and product 2 % more."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_decoder.py")
+    spec = importlib.util.spec_from_file_location("serve_decoder", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    off, draws = example.main(["--tokens", "40", "--decode", "8", "--vocab", "500"])
+    assert max(off) < 0.14
+    for last, u, token in draws:
+        host = _np(last)
+        assert token[0] == int(np.argmax(host[0]))
+        want, _, _, margin = do.sample(host[1], float(u[1]), float(np.float32(0.8)), 50, float(np.float32(0.95)))
+        assert token[1] == want or margin <= 500 * 2.0 ** -43
