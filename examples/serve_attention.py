@@ -6,7 +6,7 @@ tokens through `bpdq_linear`, `bpdq_kv_write`, `bpdq_kv_attention` and `bpdq_lin
 Weights and activations are synthetic (`workloads.py`).  Both the attention's output and the block's are compared with the same block on the
 dequantized weights in 64 bits with an exact cache.  They are compared apart because the residual is some 25 times the size of what the block
 adds here: in the sum, the residual's rounding to bfloat16 would hide what the cache and the attention do.  (Positions enter Q and K between
-the projection and the cache in a real model; that is the model's part and is left out.)
+the projection and the cache, by `bpdq_rotary`: `serve_decoder.py` has a whole decoder.)
 """
 import argparse
 import os

@@ -477,18 +477,22 @@ __device__ __forceinline__ void linear_finish_pairs(const LinearArgs& a, long to
 // Y tile of a work-group of wavefronts that share X.  What bounds it: the vector instructions that decode the weights, beside the matrix instructions, which share a SIMD's issue
 // (a stage takes about the longer of the two and 0.4 of the shorter), and the last round of tiles.  4096 bf16 tokens, 18944 x 3584 at 2 bits:
 // 517 to 612 us from card to card, some 50 of it GELU, 0.91 to 1.08 PFLOP/s (a library product of the dense 16-bit weights takes 500); 333 tokens,
-// 8192 x 8192: 100 us, 0.45 PFLOP/s (192 work-groups of 128 x 128 on 256 CUs, a wavefront to a SIMD: matrix instructions take 33 % of the busy
-// cycles, vector ones 24 %, and one does not hide the other's latency).
+// 8192 x 8192 in groups of 64: 88 us, 0.51 PFLOP/s (192 work-groups of 128 x 128 on 256 CUs, a wavefront to a SIMD, so that neither matrix nor vector
+// instructions hide the other's latency).  GATED, 2 x 18944 x 3584: 4096 bf16 tokens at 2 bits 950 to 1000 us, 1.11 to 1.17 PFLOP/s, matrix instructions
+// in 62 % of the busy cycles, vector ones in 30 % (ten rounds of work-groups for 9.25 of work); 333 fp16 tokens at 3 bits in groups of 64 132 to 140 us.
 //
 // GS: words after which a lane's group may change (of the four that it has of a chunk), VEC: the planes go by 16 bytes.
 //
 // Operands.  X comes in the order of linear_order_kernel, straight from memory into a ring of stages in LDS (LDS-DMA: no registers, no
 // instructions but the request); a row's weights for 256 columns are 16 bytes of each plane per lane (half h of a wavefront: words 4 h ..
-// of the chunk) and are decoded in registers, a step of 16 columns ahead of its products.  The levels of the rows' groups are made by
-// all threads for the next chunk and handed over in LDS.  A stage's barrier stands before its last step, when
+// of the chunk) and are decoded in registers, a step of 16 columns ahead of its products.  A stage's barrier stands before its last step, when
 // every wavefront has read the stage and the next one has landed.
+// A row belongs to one wavefront of a part, so its words and coefficients are requested into LDS by the wavefront that needs them, and its lane makes
+// the levels of its own rows.  (With the words and coefficients loaded into registers every use waited for all requests behind it, once to a group:
+// 333 tokens, 2 x 18944 x 3584 at 3 bits in groups of 64 took 165 us, 148 so; and 355 before tiles that share rows went to one XCD, whose L2 then
+// has the lines of their coefficients, of which a group takes two bytes a row: 333 tokens in groups of 128 163 and 123.)
 // The compiler does not see the LDS-DMA requests (inline assembly), so the vmcnt waits are written by hand: at most the requests of
-// the stages behind the next one may be outstanding.  Loads that the compiler issues meanwhile only make that wait longer.
+// the stages behind the next one may be outstanding.
 template <typename T, int K, typename S, int GS, bool VEC, bool GATED>
 __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a, int tok_tiles, const uint32_t* __restrict__ base) {
   constexpr int W = kWords, RT = S::RT, TT = S::TT;
@@ -498,7 +502,8 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int tid = threadIdx.x % S::kPart, lane = tid & 63, low = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % S::WR, wt = wave / S::WR;
-  // Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own: consecutive tiles, which share rows, go to one XCD.
+  // Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own: consecutive tiles, which share rows, go to one XCD.  (Not where every
+  // XCD has its own tiles of tokens anyhow: with 16 of them it makes 1 % of difference or none.)
   int tile = blockIdx.x;
   if (tok_tiles % 8 != 0) {
     const int all = gridDim.x / 8, more = gridDim.x % 8, xcd = tile % 8;

@@ -4,7 +4,9 @@
 // Angles are formed in fp64 as turns, p f / 2 pi, of which only the fraction counts: at position 10^6 an fp32 angle would be off by 0.06.  The
 // fraction, as fp32 good to 2^-26 of a turn, goes to sincospif.  A work-group makes the angles of its tokens once, in LDS, for all heads of Q and K.
 //
-// What bounds it: bytes, and for few tokens the launch.
+// What bounds it: bytes, and for few tokens the launch.  8192 fp16 tokens of 72 heads of 128 move 302 MB in 50 us (5.9 TB/s on buffers that the caches
+// hold in part, 64 us with new ones); 37 ragged chunks of 20 heads of 64, half of each turned, 74 MB in 14 us (5.2 TB/s); 16 tokens of 32 heads take 3.2 us in a graph.
+// Requests of several heads at once (two, four) cost more in registers than they gain: 51 us became 52 and 60.
 #include "common.h"
 
 namespace bpdq {

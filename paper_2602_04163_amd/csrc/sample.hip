@@ -190,14 +190,20 @@ struct SampleEight {
 // ---------------------------------------------------------------- rows cut into chunks
 //
 // A row is cut into chunks, a work-group each, in three launches, and a fourth joins them:
-//   top    the chunk's largest value and its index;
+//   top    the chunk's largest value and its index, and the largest values of its turns;
 //   hist   how far below the row's largest value its values are: a histogram over 256 steps to an octave (counts where the row asks for top-k,
-//          weights where for top-p alone);
+//          weights where for top-p alone; of the turns' largest values where these bound a small top-k);
 //   keep   from the bin where the histogram reaches its target: the sum of the weights above it, and a list of what is in it (of all down to it, where
-//          top-p follows top-k, because its target is known only when the exact top-k is);
+//          the turns' values bound it, or top-p follows top-k, whose target is known only when the exact top-k is);
 //   join   ranks the list, which gives the last one kept; then the chunk, and in it the token, where the running sum reaches u of it.
 // All comparisons behind the histogram are on (key, index) as one number, `cut` the least that is kept.  A list that would not fit (kSampleList: flat rows,
-// rows of equal values, a very large top_k before top-p) leaves the row to one work-group, which selects by radix over the row itself.
+// rows of equal values, a very large top_k before top-p) leaves the row to one work-group, which selects by radix over the row itself, some 15 passes:
+// right, but 100 to 400 us for 152064 values.
+//
+// What bounds it: the row's three readings come from the caches but for the first, so it is the chain of four launches (one bf16 row of 152064: 3.0, 4.1,
+// 4.8 and 7.2 us, where a large copy would read it in 0.1), and for many rows vector instructions, of which the fp64 exponential is some 25 a value: 64
+// fp32 rows of 152064 with mixed requests 48 us (39 MB), 256 fp16 rows of 32003 with top-p and min-p 53 us.  A border found once to a row, by
+// its last work-group behind a fence, cost more than every work-group's own search: the fence writes the L2 back (hist 19 -> 126 us).
 
 constexpr int kSampleChunkThreads = 256;
 constexpr int kSampleChunkWaves = kSampleChunkThreads / 64;
@@ -205,7 +211,7 @@ constexpr int kSampleTurn = kSampleChunkThreads * 8;      // values of a work-gr
 constexpr int kSampleChunks = 256;                        // of a row, at most
 constexpr int kSampleSteps = 3072;                        // 12 octaves of 256, from 2^-5 below the largest value to 2^7
 constexpr int kSampleList = 2048;
-constexpr int kSampleRanked = 128;                        // up to here every entry is compared with every other
+constexpr int kSampleRanked = 128;                        // up to here every entry is compared with every other (64 rows with lists of up to 940: 26 us with 512)
 
 static int sample_chunks(int n_vocab, int turns) { return bpdq_ceil_div(n_vocab + 7, turns * kSampleTurn); }        // (with the skew)
 static int sample_turns(int n_tok, int n_vocab) {         // of a chunk
