@@ -283,8 +283,8 @@ int bpdq_gated_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out
  * The sum is fp32 and is rounded once for S; Y comes from it unrounded, its squares summed in fp64, the rest fp32, Y rounded once.  A row with a
  * NaN or an infinity gets NaN (at an infinity) and zeros or NaN elsewhere; other rows do not see it.
  * S may be the residual or X, and Y may be X (same address, type and stride); other overlaps are not allowed.
- * Requirements: 1 <= d <= 65536; eps >= 2^-126; offset and eps finite; any alignment of the elements (16 bytes, strides too, is quicker).
- * n_tok = 0 launches nothing.
+ * Requirements: 1 <= d <= 65536; eps >= 2^-126; offset and eps finite; any alignment of the elements (16 bytes, strides too, is quicker); n_tok
+ * times the threads of a row (d / 16 rounded up to whole wavefronts, 1024 at most) below 2^32.  n_tok = 0 launches nothing.
  * Returns 0, or a negative code naming the argument (-1 X, -2 n_tok, -3 d, -4 ldx, -5 dtype, -6 residual, -7 ldr, -8 rdtype, -9 S, -10 lds,
  * -11 weight, -12 offset, -13 eps, -14 Y, -15 ldy). */
 int bpdq_rms_norm(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype, void* S,
@@ -339,7 +339,7 @@ int bpdq_rotary_frequencies(int rot, double base, int scaling, double factor, do
  * Of equal values the lower index comes first.  T must be above 0: any other T (a NaN too) asks for the largest value, prob 1.  top_k <= 0, top_p >= 1 or
  * NaN and min_p <= 0 or NaN keep all.  u in [0, 1); below (or NaN) counts as 0, from 1 on as the last.
  *   temperature, top_k, top_p, min_p : n_tok values each, or NULL (T = 1; nobody asks).  u : n_tok floats.
- *   token : n_tok ints;  prob : NULL or n_tok floats.
+ *   token : n_tok ints;  prob : NULL or n_tok floats.  (The workspace is some 41 KB a row.)
  * A value of minus infinity or NaN is not there; a row where nothing is there gets token -1 and prob 0.  Plus infinities share the row equally.
  * Weights are counted in units of 2^-43 of the largest (a token below half a unit is never drawn and adds nothing), their sums are exact, and the
  * result is the same from run to run.

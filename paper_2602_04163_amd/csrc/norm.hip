@@ -66,7 +66,7 @@ __device__ __forceinline__ void norm_store8(T* __restrict__ p, bool vec, int n, 
 template <typename T, typename R, int NV, bool Q8>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
   const int tid = threadIdx.x, per = blockDim.x, waves = per >> 6;
-  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  const long row = (long)blockIdx.x * blockDim.y + threadIdx.y;
   __shared__ double part_sum[16];
   __shared__ float part_most[16];
   if (row >= a.n_tok) return;                             // whole rows, which no barrier or shuffle crosses
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
       const int at = 8 * (j * per + tid);
       if (at >= a.d) break;
       const float scale = fine ? fmaxf(most[j], kNormFloor) * (1.0f / 127.0f) : __builtin_nanf("");
-      if (at % unit == 0) a.scales[(long)row * n_scale + at / unit] = scale;
+      if (at % unit == 0) a.scales[row * n_scale + at / unit] = scale;
       const float inv = 1.f / scale;
       // y / scale to the nearest whole number, ties to even, in one rounding: behind 1.5 2^23 it is the low byte (of a NaN: 0)
       uint32_t c[8], out[2];
@@ -188,7 +188,8 @@ static int norm_launch(const NormArgs& a, hipStream_t stream) {
   else
     while (per > 4 && per / 2 >= turns && 4 * per >= a.group) per /= 2;      // (a group's lanes are a row's)
   const int rows = per > 64 ? 1 : 256 / per;
-  hipLaunchKernelGGL((norm_kernel<T, R, NV, Q8>), dim3(bpdq_ceil_div(a.n_tok, rows)), dim3(per, rows), 0, stream, a);
+  if (((long)a.n_tok + rows - 1) / rows * (per * rows) > 0xffffffffL) return -2;       // threads along the grid's x
+  hipLaunchKernelGGL((norm_kernel<T, R, NV, Q8>), dim3((unsigned)(((long)a.n_tok + rows - 1) / rows)), dim3(per, rows), 0, stream, a);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }

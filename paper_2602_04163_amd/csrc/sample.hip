@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
   };
   if (bin == kSampleSteps && ask.least > 1) {             // uniform: few are likely
     // (fp32 is off by less than 2^-10 of an exponent below 2^12; further down nothing reaches min-p)
-    const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = (float)ask.per;
+    const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
     values.all([&](float v, int) {
       if (!((v - ask.most) * per < low)) add(v);
     });

@@ -54,6 +54,13 @@ def test_norms_refuse(lib, change, code):
     assert lib.bpdq_rms_norm_q8(*q8.values()) == code
 
 
+def test_norms_count_their_threads(lib):
+    """A grid ends at 2^32 threads: rows of 8192 values take 512 each, of 32 four."""
+    most = (1 << 31) - 1
+    plain = {**NORM, "Y": P, "ldy": 1 << 16, "stream": None, "n_tok": most, "d": 8192, "ldx": 8192}
+    assert lib.bpdq_rms_norm(*plain.values()) == -2
+
+
 def test_norms_refuse_outputs(lib):
     plain = {**NORM, "Y": P, "ldy": 64, "stream": None}
     for change, code in [(dict(Y=None), -14), (dict(Y=P + 1), -14), (dict(ldy=63), -15)]:

@@ -479,6 +479,33 @@ def test_sample_ties(dev):
     assert _check_sample(x, u, k=[3] * n, dev=dev) == [int(v * 3) for v in u]
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_sample_orders(dev, kind):
+    """Rows in rising and falling order, where all of the largest values lie in a few turns, and rows whose border's bin holds 65 to 4000 values."""
+    n, vocab = 8, 40000
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn((n, vocab), generator=g).sort(1).values
+    x[1::2] = x[1::2].flip(1)
+    x[4:] = 3.0 + (x[4:] * torch.tensor([0.003, 0.01, 0.03, 0.2])[:, None])
+    x[4:, 77] = 12.0
+    x, u = x.to(TYPES[kind]).to(dev), torch.rand(n, generator=g).tolist()
+    for k in (1, 7, 19, 20, 39, 40, 100, 129, 600, 3000, 39999):
+        _check_sample(x, u, k=[k] * n, dev=dev)
+        _check_sample(x, u, t=[0.7] * n, k=[k] * n, p=[0.6 + 0.04 * i for i in range(n)], dev=dev)
+    for p in (0.01, 0.2, 0.5, 0.99):
+        _check_sample(x, u, p=[p] * n, m=[0.0, 0.3] * (n // 2), dev=dev)
+
+
+def test_sample_steep(dev):
+    """Temperatures at the ends of fp32 with min-p, on values that differ by next to nothing."""
+    x = torch.zeros((4, 3000), device=dev)
+    x[:, 5::7] = -1e-45
+    x[2:, 6::7] = -1e-38
+    u = [0.3, 0.8, 0.3, 0.8]
+    _check_sample(x, u, t=[1e-40, 1e-44, 1e-40, 1e-38], m=[0.5, 0.01, 0.5, 0.3], dev=dev)
+    _check_sample(x, u, t=[3e38, 1e30, INF, 1e-45], m=[0.999, 0.01, 0.5, 0.3], dev=dev)
+
+
 def test_sample_what_is_no_number(dev):
     x = torch.randn((10, 3000), generator=torch.Generator().manual_seed(1)).to(dev)
     x[0] = -INF
