@@ -502,10 +502,9 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   const int tid = threadIdx.x % S::kPart, lane = tid & 63, low = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % S::WR, wt = wave / S::WR;
-  // Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own: consecutive tiles, which share rows, go to one XCD.  (Not where every
-  // XCD has its own tiles of tokens anyhow: with 16 of them it makes 1 % of difference or none.)
+  // Work-groups are dealt to the eight XCDs in turn, each with an L2 of its own: consecutive tiles, which share rows, go to one XCD.
   int tile = blockIdx.x;
-  if (tok_tiles % 8 != 0) {
+  if (tok_tiles > 1) {
     const int all = gridDim.x / 8, more = gridDim.x % 8, xcd = tile % 8;
     tile = xcd * all + (xcd < more ? xcd : more) + tile / 8;
   }

@@ -12,6 +12,8 @@ constexpr int kLinRowsMost = 32;                           // tokens of the kern
 //   of R = 5 and 32 tokens takes 9.5, not the 2.7 of its share.  (Of eight shapes up to 800 columns whose kernel this changes seven take
 //   0.26 to 0.94 of the time, 257 x 160 -> 20480 88 us and now 23; 1484 x 800 -> 587 takes 25 in place of 23.)
 //   tiles, per 64 columns: 256 x 256 1.25, 256 x 128 0.9, 128 x 128 in two parts 1.15 / 2, 128 x 64 in four 1.85 / 4; 8 for the order of X
+//   (256 x 256 counts 1.45: two of the others share a CU and their rounds run into one another; 512 x 3584 -> 37888 190 us with it and 158 with 256 x 128,
+//   2048 x 3584 -> 37888 at three planes 567 and 672)
 // (One, three and four planes are taken like two.)
 // 64 x 8192 -> 8192: R = 5, 2 x 16 tokens 40 us, tiles of 128 x 64 64, of 256 x 256 193; 2048 x 8192 -> 8192: 256 x 256 294, 128 x 64 535;
 // 333 x 3584 -> 18944: 256 x 128 61, 128 x 128 80, 256 x 256 86.
@@ -38,7 +40,7 @@ static inline LinearPlan linear_plan(int n_tok, int d_in, int d_out) {
   // offsets inside a row tile's planes, inside a token tile of the ordered X and so on are 32 bits in the tile kernels
   if (n_tok > kLinRowsMost && d_in <= 1 << 20) {
     const float stages = 4.f * ((d_in + 255) / 256);
-    offer(kTile256, 0, 256, 256, 1.25f * stages, 8.f);
+    offer(kTile256, 0, 256, 256, 1.45f * stages, 8.f);
     offer(kTile256x128, 0, 256, 128, 0.9f * stages, 8.f);
     offer(kTile128, 0, 128, 128, 1.15f / 2 * stages, 8.f);
     offer(kTile128x64, 0, 128, 64, 1.85f / 4 * stages, 8.f);
