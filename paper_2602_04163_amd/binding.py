@@ -471,7 +471,7 @@ def _rows(t, dtype, shape, name):
     if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
         raise BpdqError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the GPU")
     if t.is_contiguous():
-        return math.prod(shape[1:])
+        return t.numel() // shape[0] if shape[0] else math.prod(shape[1:])
     strides = t.stride()
     step = 1
     for axis in range(len(shape) - 1, 0, -1):
