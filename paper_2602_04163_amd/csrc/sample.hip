@@ -108,6 +108,17 @@ __device__ __forceinline__ u64_t sample_wave_scan(u64_t v) {
   v = join(v, sample_dpp<0x143, 0xc>(v));
   return v;
 }
+// the largest of a wavefront's, in its last lane
+__device__ __forceinline__ uint32_t sample_wave_most(uint32_t v) {
+  auto join = [&](int other) { v = v > (uint32_t)other ? v : (uint32_t)other; };
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false));
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false));
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false));
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false));
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false));
+  join(__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false));
+  return v;
+}
 __device__ __forceinline__ u64_t sample_lane(u64_t v, int lane) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane);
@@ -202,14 +213,14 @@ struct SampleEight {
 //
 // What bounds it: the row's three readings come from the caches but for the first, so it is the chain of four launches (one bf16 row of 152064: 3.0, 4.1,
 // 4.8 and 7.2 us, where a large copy would read it in 0.1), and for many rows vector instructions, of which the fp64 exponential is some 25 a value: 64
-// fp32 rows of 152064 with mixed requests 48 us (39 MB), 256 fp16 rows of 32003 with top-p and min-p 53 us.  A border found once to a row, by
+// fp32 rows of 152064 with mixed requests 47 us (39 MB), 256 fp16 rows of 32003 with top-p and min-p 51 us.  A border found once to a row, by
 // its last work-group behind a fence, cost more than every work-group's own search: the fence writes the L2 back (hist 19 -> 126 us).
 
 constexpr int kSampleChunkThreads = 256;
 constexpr int kSampleChunkWaves = kSampleChunkThreads / 64;
 constexpr int kSampleTurn = kSampleChunkThreads * 8;      // values of a work-group's turn
 constexpr int kSampleChunks = 256;                        // of a row, at most
-constexpr int kSampleSteps = 3072;                        // 12 octaves of 256, from 2^-5 below the largest value to 2^7
+constexpr int kSampleSteps = 12 * 256;                    // 12 octaves of 256, from 2^-5 below the largest value to 2^7
 constexpr int kSampleList = 2048;
 constexpr int kSampleRanked = 128;                        // up to here every entry is compared with every other (64 rows with lists of up to 940: 26 us with 512)
 
@@ -337,21 +348,26 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleA
     if (chunk == 0 && threadIdx.x == 0) w.count[row] = 0;
   }
   float most = -__builtin_inff();
-  int at = 0;
+  int best_at = 0;
+  SampleEight<T> best = values.eight;                     // the eight that have it
   float* high = w.high + (long)blockIdx.x * w.turns * kSampleChunkWaves + (threadIdx.x >> 6);
   values.eights([&](const SampleEight<T>& v, int first) {
     float here = -__builtin_inff();
-    v.all(first, [&](float x, int i) {                    // (indices rise: the first of equal ones stays)
-      at = x > most ? i : at;
-      most = fmaxf(most, x);
-      here = fmaxf(here, x);
-    });
+    v.all(first, [&](float x, int) { here = fmaxf(here, x); });
+    if (here > most) {                                    // (indices rise: the first of equal ones stays)
+      most = here;
+      best = v;
+      best_at = first;
+    }
     if (bounded) {
-      const u64_t key = sample_lane(sample_wave_scan<true>(sample_key(here)), 63);
-      if ((threadIdx.x & 63) == 0) *high = key ? sample_value((uint32_t)key) : -__builtin_inff();
+      const uint32_t key = sample_wave_most(sample_key(here));
+      if ((threadIdx.x & 63) == 63) *high = key ? sample_value(key) : -__builtin_inff();
       high += kSampleChunkWaves;
     }
   });
+  int at = 0;
+#pragma unroll
+  for (int e = 7; e >= 0; --e) at = (float)best.raw[e] == most ? best_at + e : at;
   const u64_t top = group.max(most > -__builtin_inff() ? SamplePlace<T>::of(sample_key(most), at) : 0);
   if (threadIdx.x == 0) w.top[blockIdx.x] = top;
 }
@@ -469,15 +485,16 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
     const u64_t one = sample_weight(v, ask.most, ask.per);
     sum += one >= ask.least ? one : 0;
   };
-  if (bin == kSampleSteps && ask.least > 1) {             // uniform: few are likely
-    // (fp32 is off by less than 2^-10 of an exponent below 2^12; further down nothing reaches min-p)
-    const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
-    values.all([&](float v, int) {
-      if (!((v - ask.most) * per < low)) add(v);
-    });
-  } else if (bin == kSampleSteps) {
+  // what is surely below min-p needs no weight: fp32 is off by less than 2^-10 of an exponent below 2^12, and further down nothing reaches it
+  const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
+  auto likely = [&](float v) { return !((v - ask.most) * per < low); };
+  if (bin == kSampleSteps && ask.least == 1) {            // uniform
     values.all([&](float v, int) { add(v); });
-  } else if (ask.k == 0) {
+  } else if (bin == kSampleSteps) {
+    values.all([&](float v, int) {
+      if (likely(v)) add(v);
+    });
+  } else if (ask.k == 0 && ask.least == 1) {              // most may be kept: weights without a branch
     values.eights([&](const SampleEight<T>& v, int at) {
       u64_t one[8];
       int step[8];
@@ -502,7 +519,7 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
         if (at < kSampleList) list[at] = SamplePlace<T>::of(sample_key(v), i);
         return;
       }
-      add(v);
+      if (likely(v)) add(v);
     });
   }
   sum = group.sum(sum);

@@ -310,7 +310,7 @@ def test_gated(dev, bits, group, f, d_in, n, kind, name, bias):
 
 
 # tokens, columns and pairs of rows at which each of the product's kernels is chosen (few tokens with 1, 2, 3, 5 and 8 row tiles, twice 16 tokens with
-# 2, 3 and 5, tiles of 128 x 64, 128 x 128, 256 x 128 and 256 x 256): tests/test_linear_plan.py has their rows
+# 2, 3 and 5, tiles of 128 x 64, 128 x 128, 256 x 128 and 256 x 256): tests/test_gated_kernels.py has their rows
 @pytest.mark.parametrize("n,d_in,f", [(1, 256, 1000), (65, 256, 1550), (65, 256, 2050), (700, 256, 260), (1500, 256, 65), (513, 256, 65), (257, 256, 260),
                                       (513, 256, 500), (257, 1024, 2500), (300, 512, 4100), (1025, 256, 2500), (1025, 256, 4099)])
 @pytest.mark.parametrize("bits,group,kind", [(1, 128, "bf16"), (2, 64, "f16"), (3, 32, "bf16"), (4, 128, "f16"), (2, 0, "bf16")])
