@@ -213,14 +213,17 @@ struct SampleEight {
 //
 // What bounds it: the row's three readings come from the caches but for the first, so it is the chain of four launches (one bf16 row of 152064: 3.0, 4.1,
 // 4.8 and 7.2 us, where a large copy would read it in 0.1), and for many rows vector instructions, of which the fp64 exponential is some 25 a value: 64
-// fp32 rows of 152064 with mixed requests 47 us (39 MB), 256 fp16 rows of 32003 with top-p and min-p 51 us.  A border found once to a row, by
-// its last work-group behind a fence, cost more than every work-group's own search: the fence writes the L2 back (hist 19 -> 126 us).
+// fp32 rows of 152064 with mixed requests 47 us (39 MB), 256 fp16 rows of 32003 with top-p and min-p 47 us.  A border found once to a row, by
+// its last work-group behind a fence, cost more than every work-group's own search: the fence writes the L2 back (hist 19 -> 126 us).  The search reads sums of
+// 12 bins first, 2 KB instead of 24 (256 rows of 32003: keep 16.8 -> 14.7 us, hist 16.0 -> 16.9 for making them).
 
 constexpr int kSampleChunkThreads = 256;
 constexpr int kSampleChunkWaves = kSampleChunkThreads / 64;
 constexpr int kSampleTurn = kSampleChunkThreads * 8;      // values of a work-group's turn
 constexpr int kSampleChunks = 256;                        // of a row, at most
 constexpr int kSampleSteps = 12 * 256;                    // 12 octaves of 256, from 2^-5 below the largest value to 2^7
+constexpr int kSampleShare = kSampleSteps / kSampleChunkThreads;
+static_assert(kSampleShare * kSampleChunkThreads == kSampleSteps, "whole shares");
 constexpr int kSampleList = 2048;
 constexpr int kSampleRanked = 128;                        // up to here every entry is compared with every other (64 rows with lists of up to 940: 26 us with 512)
 
@@ -244,6 +247,7 @@ struct SampleWork {
   u64_t* top;                                             // [row][chunk]
   u64_t* sum;                                             // [row][chunk]
   u64_t* hist;                                            // [row][kSampleSteps]
+  u64_t* shares;                                          // [row][kSampleChunkThreads]: sums of the histogram's, kSampleShare bins each
   float* high;                                            // [row][chunk][turn][wavefront] largest values
   u64_t* list;                                            // [row][kSampleList]
   SampleBorder* border;                                   // [row]
@@ -259,6 +263,7 @@ static size_t sample_work(SampleWork& w, void* ws, int n_tok, int n_vocab) {
   w.top = arena.take<u64_t>(n * w.chunks);
   w.sum = arena.take<u64_t>(n * w.chunks);
   w.hist = arena.take<u64_t>(n * kSampleSteps);
+  w.shares = arena.take<u64_t>(n * kSampleChunkThreads);
   w.list = arena.take<u64_t>(n * kSampleList);
   w.border = arena.take<SampleBorder>(n);
   w.high = arena.take<float>(n * w.chunks * w.turns * kSampleChunkWaves);
@@ -345,7 +350,10 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleA
   if (bounded) {
     for (int i = chunk * kSampleChunkThreads + threadIdx.x; i < kSampleSteps; i += w.chunks * kSampleChunkThreads)
       w.hist[(long)row * kSampleSteps + i] = 0;
-    if (chunk == 0 && threadIdx.x == 0) w.count[row] = 0;
+    if (chunk == 0) {
+      w.shares[(long)row * kSampleChunkThreads + threadIdx.x] = 0;
+      if (threadIdx.x == 0) w.count[row] = 0;
+    }
   }
   float most = -__builtin_inff();
   int best_at = 0;
@@ -372,16 +380,11 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_top_kernel(SampleA
   if (threadIdx.x == 0) w.top[blockIdx.x] = top;
 }
 
-// where a histogram reaches its target, by a whole work-group: hist(step) its bins; found: two words of LDS
-template <typename F>
-__device__ __forceinline__ SampleBorder sample_border(const SampleAsk& ask, u64_t top, SampleChunkGroup& group, u64_t* found, F bin_of) {
-  constexpr int kEach = kSampleSteps / kSampleChunkThreads;
-  static_assert(kEach * kSampleChunkThreads == kSampleSteps, "whole shares");
-  u64_t hist[kEach], mine = 0, total;
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) hist[e] = bin_of(threadIdx.x * kEach + e);
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) mine += hist[e];
+// where a histogram reaches its target, by a whole work-group: a thread's share of kSampleShare bins, sum_of(thread) in all; found: two words of LDS
+template <typename S, typename F>
+__device__ __forceinline__ SampleBorder sample_border(const SampleAsk& ask, u64_t top, SampleChunkGroup& group, u64_t* found, S sum_of, F bin_of) {
+  u64_t total;
+  const u64_t mine = sum_of((int)threadIdx.x);
   if (threadIdx.x == 0) found[0] = kSampleSteps;
   const u64_t run = group.scan(mine, total);
   SampleBorder s;
@@ -391,10 +394,13 @@ __device__ __forceinline__ SampleBorder sample_border(const SampleAsk& ask, u64_
   if (s.target == 0) s.target = 1;
   u64_t before = run - mine;
   if (run >= s.target && before < s.target) {
+    u64_t hist[kSampleShare];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
+    for (int e = 0; e < kSampleShare; ++e) hist[e] = bin_of(threadIdx.x * kSampleShare + e);
+#pragma unroll
+    for (int e = 0; e < kSampleShare; ++e) {
       if (before < s.target && before + hist[e] >= s.target) {
-        found[0] = threadIdx.x * kEach + e;
+        found[0] = threadIdx.x * kSampleShare + e;
         found[1] = before;
       }
       before += hist[e];
@@ -426,13 +432,19 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(Sample
   const u64_t top = sample_row_top(w, row, group);        // (its barrier is the histogram's too)
   const SampleAsk ask = sample_ask<T>(a, row, top);
   if (!ask.draw) return;                                  // uniform
+  auto share = [&](int thread) {
+    u64_t sum = 0;
+#pragma unroll
+    for (int e = 0; e < kSampleShare; ++e) sum += hist[thread * kSampleShare + e];
+    return sum;
+  };
   if (few) {
     for (int i = threadIdx.x; i < highs; i += kSampleChunkThreads) {
       const float v = w.high[(long)row * highs + i];
       if (v > -__builtin_inff()) atomicAdd(&hist[sample_step(v, ask.most)], 1ull);
     }
     __syncthreads();
-    SampleBorder border = sample_border(ask, top, group, found, [&](int i) { return hist[i]; });
+    SampleBorder border = sample_border(ask, top, group, found, share, [&](int i) { return hist[i]; });
     if (border.bin == kSampleSteps) border.bin = kSampleSteps - 1;       // fewer turns than that have values
     border.all = 1;
     if (threadIdx.x == 0) w.border[row] = border;
@@ -456,6 +468,8 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_hist_kernel(Sample
   __syncthreads();
   for (int i = threadIdx.x; i < kSampleSteps; i += kSampleChunkThreads)
     if (hist[i]) atomicAdd(&w.hist[(long)row * kSampleSteps + i], hist[i]);
+  const u64_t sum = share((int)threadIdx.x);
+  if (sum) atomicAdd(&w.shares[(long)row * kSampleChunkThreads + threadIdx.x], sum);
 }
 
 template <typename T>
@@ -474,7 +488,8 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
     border = w.border[row];
   } else {
     if (ask.draw && (ask.k || ask.p < 1.f))
-      border = sample_border(ask, top, group, found, [&](int i) { return w.hist[(long)row * kSampleSteps + i]; });
+      border = sample_border(ask, top, group, found, [&](int thread) { return w.shares[(long)row * kSampleChunkThreads + thread]; },
+                             [&](int i) { return w.hist[(long)row * kSampleSteps + i]; });
     if (chunk == 0 && threadIdx.x == 0) w.border[row] = border;
   }
   if (!ask.draw) return;                                  // uniform
