@@ -339,7 +339,7 @@ int bpdq_rotary_frequencies(int rot, double base, int scaling, double factor, do
  * Of equal values the lower index comes first.  T must be above 0: any other T (a NaN too) asks for the largest value, prob 1.  top_k <= 0, top_p >= 1 or
  * NaN and min_p <= 0 or NaN keep all.  u in [0, 1); below (or NaN) counts as 0, from 1 on as the last.
  *   temperature, top_k, top_p, min_p : n_tok values each, or NULL (T = 1; nobody asks).  u : n_tok floats.
- *   token : n_tok ints;  prob : NULL or n_tok floats.  (The workspace is some 41 KB a row.)
+ *   token : n_tok ints;  prob : NULL or n_tok floats.  (The workspace is some 43 KB a row.)
  * A value of minus infinity or NaN is not there; a row where nothing is there gets token -1 and prob 0.  Plus infinities share the row equally.
  * Weights are counted in units of 2^-43 of the largest (a token below half a unit is never drawn and adds nothing), their sums are exact, and the
  * result is the same from run to run.
