@@ -560,6 +560,20 @@ def test_sample_strides(dev, kind):
     assert bq.bpdq_sample(x[:0], u[:0]).shape == (0,)
 
 
+def test_sample_borders_everywhere(dev):
+    """Values whose distances from the largest pass through every step of the histogram, kept up to any of them.  Weights are equal up to 2^-22 (distances
+    are below 128, the temperature 10^9), so that top-p keeps the k that top_p = (k - 1/2) / n asks for, and the last kept has more than u leaves."""
+    n, vocab = 1024, 8192
+    x = torch.zeros(vocab, dtype=torch.float64)
+    x[1:] = -torch.exp2(-5 + 12 * torch.arange(vocab - 1) / vocab)
+    x = x.float().to(dev).repeat(n, 1)
+    k = torch.arange(n, dtype=torch.int32) * 8 + torch.arange(n, dtype=torch.int32) % 8 + 1
+    u, t = torch.full((n,), 1 - 2.0 ** -24, device=dev), torch.full((n,), 1e9, device=dev)
+    assert torch.equal(bq.bpdq_sample(x, u, temperature=t, top_k=k.to(dev)).cpu(), k - 1)
+    p = ((k.double() - 0.5) / vocab).float().to(dev)
+    assert torch.equal(bq.bpdq_sample(x, u, temperature=t, top_p=p).cpu(), k - 1)
+
+
 def test_sample_largest_vocabulary(dev):
     x = torch.zeros((2, 1 << 20), dtype=torch.float16, device=dev)
     x[1, -1] = 30.0
