@@ -500,8 +500,9 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
     const u64_t one = sample_weight(v, ask.most, ask.per);
     sum += one >= ask.least ? one : 0;
   };
-  // what is surely below min-p needs no weight: fp32 is off by less than 2^-10 of an exponent below 2^12, and further down nothing reaches it
-  const float low = log2f((float)ask.least) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
+  // what surely weighs less than min-p leaves needs no weight: one of `least` units begins half a unit below, and fp32 is off by less than 2^-10 of an
+  // exponent below 2^12, where further down nothing reaches it
+  const float low = log2f((float)ask.least - 0.5f) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
   auto likely = [&](float v) { return !((v - ask.most) * per < low); };
   if (bin == kSampleSteps && ask.least == 1) {            // uniform
     values.all([&](float v, int) { add(v); });
