@@ -501,9 +501,9 @@ __global__ __launch_bounds__(kSampleChunkThreads) void sample_keep_kernel(Sample
     sum += one >= ask.least ? one : 0;
   };
   // what surely weighs less than min-p leaves needs no weight: one of `least` units begins half a unit below, and fp32 is off by less than 2^-10 of an
-  // exponent below 2^12, where further down nothing reaches it
-  const float low = log2f((float)ask.least - 0.5f) - 43.f - 0x1p-8f, per = fminf((float)ask.per, 3.4e38f);
-  auto likely = [&](float v) { return !((v - ask.most) * per < low); };
+  // exponent below 2^12, where further down nothing reaches it.  (Halves: the distance of two fp32 values may be twice fp32's largest.)
+  const float low = log2f((float)ask.least - 0.5f) - 43.f - 0x1p-8f, per = (float)fmin(2.0 * ask.per, 3.4e38), half = 0.5f * ask.most;
+  auto likely = [&](float v) { return !(fmaf(0.5f, v, -half) * per < low); };
   if (bin == kSampleSteps && ask.least == 1) {            // uniform
     values.all([&](float v, int) { add(v); });
   } else if (bin == kSampleSteps) {

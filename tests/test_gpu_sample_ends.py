@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2602_04163_amd import binding as bq
-from test_gpu_decoder import E, INF, dev  # noqa: F401
+from test_gpu_decoder import E, INF, _check_sample, dev  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,14 @@ def test_sample_keeps_what_rounds_to_min_p(dev, units):  # noqa: F811
         token, prob = _last_of(x, dev, min_p=units * 2.0 ** -43, **asked)
         assert (token == 3800).all(), (asked, token)
         assert ((prob - units * 2.0 ** -43).abs() <= 4 * E * units * 2.0 ** -43).all()
+
+
+def test_sample_distances_beyond_fp32(dev):  # noqa: F811
+    """Values whose difference is infinite in fp32, at temperatures at which both count."""
+    x = torch.full((6, 40), -3e38, device=dev)
+    x[:, [1, 20]] = 3e38
+    x[:, 30] = 0.0
+    u = [0.0, 0.02, 0.13, 0.4, 0.7, 0.99]
+    for t in (3e38, 1e38, 3e37):
+        for asked in (dict(m=[0.001] * 6), dict(k=[35] * 6), dict(k=[30] * 6, m=[0.05] * 6), dict(p=[0.9] * 6, m=[0.001] * 6)):
+            _check_sample(x, u, t=[t] * 6, dev=dev, **asked)
