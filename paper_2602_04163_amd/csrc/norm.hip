@@ -111,16 +111,25 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
     sum = 0.0;
     for (int q = 0; q < waves; ++q) sum += part_sum[q];
   }
-  const float inv_rms = (float)rsqrt(sum / a.d + (double)a.eps);
+  double inv_rms = rsqrt(sum / a.d + (double)a.eps);
   if (a.sum) {
     R* s = static_cast<R*>(a.sum) + row * a.lds;
 #pragma unroll
     for (int j = 0; j < NV; ++j) norm_store8(s + 8 * (j * per + tid), a.vec_s, a.d - 8 * (j * per + tid), v[j]);
   }
+  if (inv_rms < 0x1p-120) {                               // (the same for all of a row) as fp32 it would lose bits
+    inv_rms *= 0x1p16;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] *= 0x1p-16f;
+  }
+  // (the value over the root, at most 256, first: root and weight together may leave fp32 either way)
+  const float by = (float)inv_rms;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] *= inv_rms * (a.offset + (float)w[j].raw[e]);
+    for (int e = 0; e < 8; ++e) v[j][e] = v[j][e] * by * (a.offset + (float)w[j].raw[e]);
   if constexpr (!Q8) {
     T* y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
