@@ -291,7 +291,8 @@ int bpdq_rms_norm(const void* X, int n_tok, int d, long ldx, int dtype, const vo
                   long lds, const void* weight, float offset, float eps, void* Y, long ldy, void* stream);
 /* The same with Y in 8 bits, as it is kept or sent: codes[t][c] = rint(y / scale) in [-127, 127] (row stride ldc), y before any rounding, with one scale
  * for a row (group = 0) or for each `group` (32, 64, 128 or 256, a divisor of d) of its channels: scales[t][c / group], dense,
- * max(amax, 2^-96) * (1/127), amax the largest |y| of the group.  A row with a NaN or an infinity gets scales of NaN.
+ * max(amax, 2^-96) * (1/127), amax the largest |y| of the group.  A row with a NaN or an infinity gets scales of NaN, and so does a group with a y that
+ * is NaN or infinite by its weight; codes under a scale of NaN say nothing.
  * Returns as above (-14 group, -15 codes, -16 ldc, -17 scales). */
 int bpdq_rms_norm_q8(const void* X, int n_tok, int d, long ldx, int dtype, const void* residual, long ldr, int rdtype, void* S,
                      long lds, const void* weight, float offset, float eps, int group, int8_t* codes, long ldc, float* scales,

@@ -135,29 +135,29 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) norm_store8(y + 8 * (j * per + tid), a.vec_y, a.d - 8 * (j * per + tid), v[j]);
   } else {
-    // (values behind the row's end are zero, whatever the weight; a maximum leaves out what is no number: the sum has it)
+    // (values behind the row's end are zero, whatever the weight; a maximum that a NaN goes through, as it may be the weight's alone)
     float most[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       most[j] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most[j] = fmaxf(most[j], fabsf(v[j][e]));
+      for (int e = 0; e < 8; ++e) most[j] = __builtin_elementwise_maximum(most[j], fabsf(v[j][e]));
     }
     if (a.group == 0) {
 #pragma unroll
-      for (int j = 1; j < NV; ++j) most[0] = fmaxf(most[0], most[j]);
-      for (int o = lanes >> 1; o > 0; o >>= 1) most[0] = fmaxf(most[0], __shfl_xor(most[0], o, 64));
+      for (int j = 1; j < NV; ++j) most[0] = __builtin_elementwise_maximum(most[0], most[j]);
+      for (int o = lanes >> 1; o > 0; o >>= 1) most[0] = __builtin_elementwise_maximum(most[0], __shfl_xor(most[0], o, 64));
       if (waves > 1) {
         if ((tid & 63) == 0) part_most[tid >> 6] = most[0];
         __syncthreads();
-        for (int q = 0; q < waves; ++q) most[0] = fmaxf(most[0], part_most[q]);
+        for (int q = 0; q < waves; ++q) most[0] = __builtin_elementwise_maximum(most[0], part_most[q]);
       }
 #pragma unroll
       for (int j = 1; j < NV; ++j) most[j] = most[0];
     } else {
       for (int o = a.group / 16; o > 0; o >>= 1) {        // (a group is 4 to 32 lanes, and no more than a row's)
 #pragma unroll
-        for (int j = 0; j < NV; ++j) most[j] = fmaxf(most[j], __shfl_xor(most[j], o, 64));
+        for (int j = 0; j < NV; ++j) most[j] = __builtin_elementwise_maximum(most[j], __shfl_xor(most[j], o, 64));
       }
     }
     const int unit = a.group ? a.group : a.d, n_scale = a.group ? a.d / a.group : 1;
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
     for (int j = 0; j < NV; ++j) {
       const int at = 8 * (j * per + tid);
       if (at >= a.d) break;
-      const float scale = fine ? fmaxf(most[j], kNormFloor) * (1.0f / 127.0f) : __builtin_nanf("");
+      const float scale = fine && most[j] < __builtin_inff() ? fmaxf(most[j], kNormFloor) * (1.0f / 127.0f) : __builtin_nanf("");
       if (at % unit == 0) a.scales[row * n_scale + at / unit] = scale;
       const float inv = 1.f / scale;
-      // y / scale to the nearest whole number, ties to even, in one rounding: behind 1.5 2^23 it is the low byte (of a NaN: 0)
+      // y / scale to the nearest whole number, ties to even, in one rounding: behind 1.5 2^23 it is the low byte (under a scale of NaN: any)
       uint32_t c[8], out[2];
 #pragma unroll
       for (int e = 0; e < 8; ++e) c[e] = __builtin_bit_cast(uint32_t, fmaf(v[j][e], inv, 0x1.8p23f));
