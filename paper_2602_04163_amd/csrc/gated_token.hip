@@ -71,6 +71,7 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
   extern __shared__ float lds[];
   float* T = lds;                                        // [8][W][16][64], at LDS address 0: the kernel has no other LDS
   float* Sw = lds + 8 * W * 16 * 64;                     // [W][64]: sum of x over each word
+  int* size_s = reinterpret_cast<int*>(Sw + W * 64);     // [wavefront]: of its values of x
   constexpr int kSegs = 8 * W, kSegPerThread = (kSegs + kGemvWaves - 1) / kGemvWaves;
   const int nw = a.d_in / 32, n_grp = a.d_in / a.group, wpg = a.group / 32, half = a.d_out / 2;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -86,42 +87,63 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
     gemv_fetch<K, W, NG, ROWS, STRIDED, true>(a.planes, a.coefs, a.d_out, nw, n_grp, wpg, f + (ROWS == 1 && item % 2 ? half : 0), 0, nw, lane,
                                               at, it);
   };
-  // x of the table's segments: bf16 under 2^-24, so that sums of its largest values stay finite
+  // x of the table's segments
   const unsigned short* x = static_cast<const unsigned short*>(a.x);
-  float4 xv[kSegPerThread];
+  unsigned short h[kSegPerThread][4];
 #pragma unroll
   for (int s = 0; s < kSegPerThread; ++s) {
     const int id = wave + kGemvWaves * s;                // segment (q, j) = (id / W, id % W)
     const int wl = STRIDED ? 64 * (id % W) + lane : W * lane + id % W;
-    const bool in = id < kSegs && wl < nw;
-    const unsigned short* p = x + (in ? 32 * wl + 4 * (id / W) : 0);
-    unsigned short h[4];
-    if (a.vec_x) *reinterpret_cast<uint2*>(h) = *reinterpret_cast<const uint2*>(p);
+    const unsigned short* p = x + (id < kSegs && wl < nw ? 32 * wl + 4 * (id / W) : 0);
+    if (a.vec_x) *reinterpret_cast<uint2*>(h[s]) = *reinterpret_cast<const uint2*>(p);
     else
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = p[e];
+      for (int e = 0; e < 4; ++e) h[s][e] = p[e];
+  }
+  fetch(0, cur);                                         // (asked for before x is looked at)
+  float4 xv[kSegPerThread];
+#pragma unroll
+  for (int s = 0; s < kSegPerThread; ++s) {
+    const int id = wave + kGemvWaves * s, wl = STRIDED ? 64 * (id % W) + lane : W * lane + id % W;
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[e] = bf16 ? __builtin_bit_cast(float, (uint32_t)h[e] << 16) * 0x1p-24f : (float)__builtin_bit_cast(_Float16, h[e]);
-      v[e] = in ? v[e] : 0.f;
+      v[e] = bf16 ? __builtin_bit_cast(float, (uint32_t)h[s][e] << 16) : (float)__builtin_bit_cast(_Float16, h[s][e]);
+      v[e] = id < kSegs && wl < nw ? v[e] : 0.f;
     }
     xv[s] = make_float4(v[0], v[1], v[2], v[3]);
   }
-  fetch(0, cur);
+  // A bf16 token whose largest value is 2^64 or more, or below 2^-24, is taken times a power of two, in tables made anew: its sums would leave fp32,
+  // or lose bits among fp32's denormals.
+  if (bf16) {
+    float most = 0.f;
 #pragma unroll
-  for (int s = 0; s < kSegPerThread; ++s) {
-    const int id = wave + kGemvWaves * s;
-    if (id < kSegs) gemv_table(xv[s], T + id * 16 * 64 + lane);
+    for (int s = 0; s < kSegPerThread; ++s)
+      most = fmaxf(most, fmaxf(fmaxf(fabsf(xv[s].x), fabsf(xv[s].y)), fmaxf(fabsf(xv[s].z), fabsf(xv[s].w))));
+    const bool large = __any(most >= 0x1p64f), small = !__any(most >= 0x1p-24f);
+    if (lane == 0) size_s[wave] = large ? 2 : small ? 0 : 1;
   }
-  __syncthreads();
-  if (tid < 64 * W) {
-    float sw = 0.f;
+  float scale = 1.f, unscale = 1.f;
+  for (;;) {                                             // once, or twice
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sw += T[((q * W + (tid >> 6)) * 16 + 15) * 64 + lane];
-    Sw[tid] = sw;
+    for (int s = 0; s < kSegPerThread; ++s) {
+      const int id = wave + kGemvWaves * s;
+      if (id < kSegs) gemv_table(make_float4(xv[s].x * scale, xv[s].y * scale, xv[s].z * scale, xv[s].w * scale), T + id * 16 * 64 + lane);
+    }
+    __syncthreads();
+    const int size = size_s[lane & (kGemvWaves - 1)];
+    if (tid < 64 * W) {
+      float sw = 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sw += T[((q * W + (tid >> 6)) * 16 + 15) * 64 + lane];
+      Sw[tid] = sw;
+    }
+    __syncthreads();
+    const bool large = __any(size == 2), small = !__any(size > 0);
+    if (!bf16 || scale != 1.f || !(large || small)) break;       // uniform over the work-group
+    scale = large ? 0x1p-88f : 0x1p100f;
+    unscale = large ? 0x1p88f : 0x1p-100f;
   }
-  __syncthreads();
   // the first item is here: or the look-ups below, reached with and without a request ahead of them, would wait for
   // everything in flight (vmcnt 0; the other counters at their maxima)
   __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -143,10 +165,8 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
     }
     float up = v[ROWS - 1];
     if (ROWS == 2) gate = v[0];
-    if (bf16) {
-      gate *= 0x1p24f;
-      up *= 0x1p24f;
-    }
+    gate *= unscale;
+    up *= unscale;
     if (lane == 0) {
       if (a.bias) {
         const unsigned short g = static_cast<const unsigned short*>(a.bias)[f], u = static_cast<const unsigned short*>(a.bias)[half + f];
@@ -160,14 +180,17 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
   }
 }
 
+template <int W>
+constexpr size_t gated_lds_bytes() { return gemv_lds_bytes<W>() + kGemvWaves * sizeof(int); }
+
 // Items of both rows where two of them, this one and the next, fit the 128 registers of a 1024-thread work-group.
 template <int K, int W, int NG, bool STRIDED>
 static int gated_token_launch(const LinearArgs& a, int bf16, hipStream_t stream) {
   constexpr int kRegs = K * W + (K + 1) * (!STRIDED && NG > 1 ? NG / 2 : NG), ROWS = kRegs <= 21 ? 2 : 1;
-  BPDQ_HIP_TRY((bpdq_lds_limit<&gated_token_kernel<K, W, NG, ROWS, STRIDED>>(gemv_lds_bytes<W>())));
+  BPDQ_HIP_TRY((bpdq_lds_limit<&gated_token_kernel<K, W, NG, ROWS, STRIDED>>(gated_lds_bytes<W>())));
   const int units = bpdq_ceil_div(a.d_out / 2, kGemvWaves), passes = bpdq_ceil_div(units, 256);
   hipLaunchKernelGGL((gated_token_kernel<K, W, NG, ROWS, STRIDED>), dim3(bpdq_ceil_div(units, passes)), dim3(kGemvThreads),
-                     gemv_lds_bytes<W>(), stream, a, bf16, passes);
+                     gated_lds_bytes<W>(), stream, a, bf16, passes);
   BPDQ_LAUNCH_CHECK();
   return 0;
 }
