@@ -356,16 +356,18 @@ struct LinearTile {
   static constexpr int kDma = kToks * 128 / 1024 / (WR * WT);       // requests of a wavefront per 64 columns
   static constexpr int kStage = kToks * 128;             // bytes of 64 columns of X
   static constexpr int kRing = kStages * KS * kStage;
-  // a wavefront's own: the coefficients of a group of its rows, and its words, of four to a lane or, where these do not fit, of one
+  // a wavefront's own: the coefficients of a group of its rows, and its words, four to a lane, of all its blocks of rows or, where these do not
+  // fit, of one block after the other
   static constexpr int kWaves = kThreads / 64;
   static constexpr int kCoefs = (K + 1) * RT * 256;
-  static constexpr bool kFour = kRing + kWaves * (kCoefs + K * RT * 1024) <= 160 * 1024;
-  static constexpr int kWordBytes = K * RT * (kFour ? 1024 : 256);
+  static constexpr int kTurns = kRing + kWaves * (kCoefs + K * RT * 1024) <= 160 * 1024 ? 1 : RT;
+  static constexpr int kWordBytes = K * RT / kTurns * 1024;
   static constexpr size_t kLds = (size_t)kRing + kWaves * (kCoefs + kWordBytes);
   static_assert(WT == 1, "a row belongs to one wavefront of a part");
   static_assert(kDma % 4 == 0, "a quarter with each step");
   static_assert(kStages >= 3, "the requests of a stage are spread over the one before");
   static_assert(kLds <= 160 * 1024, "one work-group to a CU");
+  static_assert(kTurns == 1 || (kTurns == 2 && WR * WT * kWordBytes <= kStage), "the second block's first words wait in the ring's last slot");
   static_assert(KS == 1 || (size_t)(KS / 2) * kRows * kToks * 4 <= kLds, "the joining of the parts has to fit");
 };
 
@@ -550,21 +552,21 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
   }
   // Words and coefficients go through LDS too, by the wavefront that needs them, so that every load of the loop is a request whose wait is
   // counted: a load into registers would wait for all requests behind it (the compiler does not count these).
-  constexpr bool kFour = VEC && S::kFour;                // four words at a time (of a chunk), or one (of a stage)
-  constexpr int kW = kFour ? W : 1;
+  constexpr int kW = VEC ? W : 1;                        // four words at a time (of a chunk), or one (of a stage)
+  constexpr int kTurns = VEC ? S::kTurns : 1, kBlocks = RT / kTurns;       // blocks of rows whose words are in LDS at once
   const unsigned own = (unsigned)(S::kRing + (part * (S::kPart / 64) + wave) * (S::kCoefs + S::kWordBytes));
   const char* own_c = lds + own + 4 * lane;
-  const char* own_w = lds + own + S::kCoefs + (kFour ? 16 : 4) * lane;
   auto level_word = [&](int stage) { return 2 * W * (stage / W * S::KS + part) + W * half + stage % W; };
-  auto request_w = [&](int stage) {                      // words past the end: the row's first, under levels of zero
+  const unsigned own_w = own + S::kCoefs;
+  auto request_w = [&](int stage, int turn, unsigned to) {           // words past the end: the row's first, under levels of zero
     const int word = level_word(stage);
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
       for (int i = 0; i < K; ++i) {
-        const unsigned voff = (row[r] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u;
-        if constexpr (kFour) lds_dma_1k(w_base[i], voff, own + S::kCoefs + (r * K + i) * 1024);
-        else lds_dma_dword(w_base[i], voff, own + S::kCoefs + (r * K + i) * 256);
+        const unsigned voff = (row[turn * kBlocks + b] * (unsigned)nw + (unsigned)(word < nw ? word : 0)) * 4u;
+        if constexpr (VEC) lds_dma_1k(w_base[i], voff, to + (b * K + i) * 1024);
+        else lds_dma_dword(w_base[i], voff, to + (b * K + i) * 256);
       }
   };
   auto request_c = [&](int stage) {                      // of the group that begins with the stage's word
@@ -576,17 +578,18 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       for (int i = 0; i <= K; ++i) lds_dma_ushort(c_base[i], (row[r] * (unsigned)n_grp + g) * 2u, own + (r * (K + 1) + i) * 256);
   };
   uint32_t w_cur[RT][K][kW], w_next[RT][K][kW];
-  auto read_w = [&](uint32_t (&w)[RT][K][kW]) {
+  auto read_w = [&](uint32_t (&w)[RT][K][kW], int turn, unsigned from) {
+    const char* p = lds + from + (VEC ? 16 : 4) * lane;
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
       for (int i = 0; i < K; ++i) {
-        if constexpr (kFour) {
-          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(own_w + (r * K + i) * 1024);
+        if constexpr (VEC) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p + (b * K + i) * 1024);
 #pragma unroll
-          for (int j = 0; j < W; ++j) w[r][i][j] = v[j];
+          for (int j = 0; j < W; ++j) w[turn * kBlocks + b][i][j] = v[j];
         } else {
-          w[r][i][0] = *reinterpret_cast<const uint32_t*>(own_w + (r * K + i) * 256);
+          w[turn * kBlocks + b][i][0] = *reinterpret_cast<const uint32_t*>(p + (b * K + i) * 256);
         }
       }
   };
@@ -630,12 +633,14 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int r = 0; r < RT; ++r) {
       uint32_t words[K];
 #pragma unroll
-      for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][kFour ? j : 0];
+      for (int i = 0; i < K; ++i) words[i] = w_cur[r][i][VEC ? j : 0];
       v[f & 1][r] = PlaneWord<K>(words).values(levels[r], f);
     }
   };
 
-  request_w(0);
+  const unsigned spare = (unsigned)((part * S::kStages + S::kStages - 1) * S::kStage + wave * S::kWordBytes);      // in the slot requested last
+  request_w(0, 0, own_w);
+  if (kTurns > 1) request_w(0, 1, spare);
   request_c(0);
 #pragma unroll
   for (int s = 0; s < S::kStages - 1; ++s)
@@ -643,12 +648,14 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
     for (int q = 0; q < 4; ++q) request(s, s, q);
   wait_vm<(S::kStages - 1) * S::kDma>();
   asm volatile("" ::: "memory");                         // reads of LDS stay behind the wait
-  read_w(w_cur);
+  read_w(w_cur, 0, own_w);
+  if (kTurns > 1) read_w(w_cur, 1, spare);
   read_c();
   make_levels(levels, 0);
   wait_vm<(S::kStages - 2) * S::kDma>();
   __syncthreads();                                       // (reads of LDS have their data before it)
-  if (!kFour) request_w(1);
+  if (!VEC) request_w(1, 0, own_w);
+  if (kTurns > 1) request_w(W, 0, own_w);
   request_c(GS);
   request(S::kStages - 1, S::kStages - 1, 0);
 #pragma unroll
@@ -663,14 +670,15 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
       for (int f = 0; f < 4; ++f) {
         // the next words and coefficients, where they landed a stage ago: beside these products
         const bool turn = (j + 1) % GS == 0;             // the next stage's word begins a group
-        if (kFour && j + 1 == W && f == 0) read_w(w_next);
+        if (kTurns > 1 && j == 1 && f == 0) read_w(w_next, 0, own_w);
+        if (VEC && j + 1 == W && f == 0) read_w(w_next, kTurns - 1, own_w);
         if (GS > 1 && turn && f == 0) read_c();
         if (GS > 1 && turn && f == 1) make_levels(levels_next, stage + 1);
         if (f == 3) {
           wait_vm<(S::kStages - 2) * S::kDma>();
           asm volatile("" ::: "memory");
-          if (!kFour) read_w(w_next);
-          if (!kFour || j + 1 == W) {
+          if (!VEC) read_w(w_next, 0, own_w);
+          if (!VEC || j + 1 == W) {
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -689,7 +697,10 @@ __global__ __launch_bounds__(S::kThreads) void linear_tiles_kernel(LinearArgs a,
           __syncthreads();
           // (before the stage's first requests, so that the next stage's wait is one for these; a chunk's words a stage behind its
           // coefficients, so that the wavefront is held up by fewer requests at once)
-          if (!kFour || j == 0) request_w(kFour ? stage - j + W : stage + 2);
+          if (!VEC) request_w(stage + 2, 0, own_w);
+          else if (kTurns == 1 && j == 0) request_w(stage + W, 0, own_w);
+          else if (kTurns > 1 && j == 1) request_w(stage - j + W, 1, own_w);
+          else if (kTurns > 1 && j + 1 == W) request_w(stage + 1 + W, 0, own_w);
           if (turn) request_c(stage + 1 + GS);
         }
         // the slot of the stage before is free behind its barrier
