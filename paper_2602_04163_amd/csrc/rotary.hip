@@ -14,7 +14,7 @@ namespace bpdq {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kRotThreads = 256;
-constexpr int kRotPer = 8;                                // tokens of a work-group at most
+constexpr int kRotPer = 4;                                // tokens of a work-group at most
 constexpr int kRotDimMost = 512;
 
 struct RotaryArgs {
@@ -234,8 +234,8 @@ extern "C" int bpdq_rotary(const double* freq, int rot, int layout, float mscale
   a.copy_k = K_out != K;
   a.mscale = mscale;
   a.sign = inverse ? -1.f : 1.f;
-  a.per = 4;
-  if ((long)bpdq_ceil_div(a.max_tok, 4) * n_seq < 1024) a.per = 1;
+  a.per = kRotPer;
+  if ((long)bpdq_ceil_div(a.max_tok, kRotPer) * n_seq < 1024) a.per = 1;
   if ((long)bpdq_ceil_div(a.max_tok, a.per) * kRotThreads > 0xffffffffL) return -10;           // threads along the grid's x
   hipStream_t stream = static_cast<hipStream_t>(stream_);
   if (dtype == BPDQ_F32) return rotary_launch<float>(a, n_seq, stream);
