@@ -268,7 +268,8 @@ int bpdq_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int 
  * f < d_out, from two layers stacked by rows (2 d_out rows, gate first), as bpdq_quantize_layers leaves layers that share one input.
  *   planes : [bits][2 d_out][d_in/32];  coefs_h : [bits+1][2 d_out][d_in/group];  bias : 2 d_out values or NULL;  Y : n_tok x d_out, row stride ldy.
  * Types, activations, precision, workspace (bpdq_linear_workspace_bytes) and requirements are those of bpdq_linear; neither projection is rounded
- * before the product.  Y must not overlap X.  A plane (2 d_out x d_in bits) has to be below 4 GiB.
+ * before the product.  (One token of up to 8192 columns: weights are not rounded to fp16 either, and X in bf16 keeps all its bits, so its result is a little
+ * nearer than that of the same token among others.)  Y must not overlap X.  A plane (2 d_out x d_in bits) has to be below 4 GiB.
  * Returns 0, or a negative code naming the argument (-1 planes, -2 coefs_h, -3 d_out, -4 d_in, -5 bits, -6 group, -7 X,
  * -8 n_tok, -9 ldx, -10 dtype, -11 bias, -12 act, -13 Y, -14 ldy, -15 ws, -16 ws_bytes). */
 int bpdq_gated_linear(const uint32_t* planes, const uint16_t* coefs_h, int d_out, int d_in, int bits, int group,

@@ -1,7 +1,7 @@
 // The gated product (linear.h) for one token: the look-ups of gemv.hip, gate and up row of a value by the same wavefront.
 //
 // What bounds it: the look-ups' vector instructions and LDS reads beside the memory, as there.  2 x 18944 x 3584 at 2 bits in groups of 128, one
-// bf16 token: 13.5 us (40 MB, 3.0 TB/s); the few-token kernel of the matrix instructions (linear.h) takes 26, since it decodes weights that one token
+// bf16 token: 13.7 us (40 MB, 2.9 TB/s); the few-token kernel of the matrix instructions (linear.h) takes 26, since it decodes weights that one token
 // uses once.  Sums are of exact products in fp32, so a weight is not rounded to fp16 here.
 #include "gemv.h"
 #include "linear.h"

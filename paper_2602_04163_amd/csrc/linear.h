@@ -70,13 +70,13 @@ __device__ __forceinline__ uint32_t linear_most(u32x4_t v, uint32_t most) {
   }
   return most;
 }
-// eight consecutive values of X
 // GATED: the rows are those of two projections, gate and then up, of `half` rows each, and a tile takes them by eights in turn, so that
 // the eight of a gate and the eight of its up meet in one wavefront's epilogue.  The stored row of a tile's row v (past the end: the last):
 __device__ __forceinline__ int linear_pair_row(int v, int half) {
   const int f = (v >> 4) * 8 + (v & 7);
   return (f < half ? f : half - 1) + (v & 8 ? half : 0);
 }
+// eight consecutive values of X
 template <typename T>
 __device__ __forceinline__ u32x4_t linear_load8(const T* __restrict__ x, bool vec) {
   if (vec) return *reinterpret_cast<const u32x4_t*>(x);

@@ -12,11 +12,13 @@ constexpr int kLinRowsMost = 32;                           // tokens of the kern
 //   of R = 5 and 32 tokens takes 9.5, not the 2.7 of its share.  (Of eight shapes up to 800 columns whose kernel this changes seven take
 //   0.26 to 0.94 of the time, 257 x 160 -> 20480 88 us and now 23; 1484 x 800 -> 587 takes 25 in place of 23.)
 //   tiles, per 64 columns: 256 x 256 1.25, 256 x 128 0.9, 128 x 128 in two parts 1.15 / 2, 128 x 64 in four 1.85 / 4; 8 for the order of X
-//   (256 x 256 counts 1.45: two of the others share a CU and their rounds run into one another; 512 x 3584 -> 37888 190 us with it and 158 with 256 x 128,
-//   2048 x 3584 -> 37888 at three planes 567 and 672)
+//   (256 x 256 counts 1.45: two of the others share a CU and their rounds run into one another.  Fp16, two planes in groups of 128, with it and with
+//   256 x 128, which its estimate then takes: 512 x 3584 -> 37888 194 us and 160, 1024 x 3584 -> 18944 195 and 162, 700 x 8192 -> 29568 402 and 368, 3000 x 8192 -> 8192 427
+//   and 417; at three planes in groups of 32 1024 x 3584 -> 18944 291 and 280, at four in groups of 128 230 and 240.  2048 x 3584 -> 37888 keeps
+//   it: 530 and 554.)
 // (One, three and four planes are taken like two.)
-// 64 x 8192 -> 8192: R = 5, 2 x 16 tokens 40 us, tiles of 128 x 64 64, of 256 x 256 193; 2048 x 8192 -> 8192: 256 x 256 294, 128 x 64 535;
-// 333 x 3584 -> 18944: 256 x 128 61, 128 x 128 80, 256 x 256 86.
+// 64 x 8192 -> 8192: R = 5, 2 x 16 tokens 43 us, tiles of 128 x 64 48, of 256 x 256 160; 2048 x 8192 -> 8192: 256 x 256 263, 128 x 64 432;
+// 333 x 3584 -> 18944: 256 x 128 62, 128 x 128 72, 256 x 256 86.
 enum LinearKernel { kRows1, kRows2, kTile256, kTile256x128, kTile128, kTile128x64 };
 struct LinearPlan {
   int kernel, r;

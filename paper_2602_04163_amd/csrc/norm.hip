@@ -6,7 +6,7 @@
 // unrounded sum.
 //
 // What bounds it: bytes, and for few rows the launch.  4096 bf16 rows of 8192 with an fp32 residual move 403 MB in 74 us (5.4 TB/s; a large copy
-// reaches 4.9 to 5.3 from card to card); 16 x 3584 takes 3.2 us in a graph, 3.9 alone, 100000 x 128 10.  To codes vector instructions bound it, some 25 a value and 74 % of the
+// reaches 4.9 to 5.3 from card to card); 16 x 3584 takes 3.5 us in a graph, 3.9 alone, 100000 x 128 10.  To codes vector instructions bound it, some 25 a value and 74 % of the
 // busy cycles, conversions to and from fp64 among them: 1023 x 18944 in groups of 128 20 us for 58 MB (2.9 TB/s).
 #include "common.h"
 
@@ -203,9 +203,11 @@ static int norm_launch(const NormArgs& a, hipStream_t stream) {
   return 0;
 }
 
-// Turns of a thread, measured (us; bf16, with a residual in bf16, back to back in a graph): few rows want threads, 16 x 3584 3.2 with one
-// turn, 3.8 with two, but 333 x 8192 6.4 and 5.5; many rows two, 4096 x 8192 + fp32 79 with one, 74 with two and with four; wide rows so many that a
-// CU holds more than two of them: 1023 x 18944 to codes 24 with four turns (640 threads), 19 with five (512), 21 with six, 32 with eight.
+// Turns of a thread, measured (us; bf16, with a residual in bf16, back to back in a graph): few rows want threads, 16 x 3584 3.5 with one
+// turn, 3.8 with two, but 333 x 8192 6.4 and 5.5; many rows two, 4096 x 8192 + fp32 79 with one, 75 with two and with four; wide rows so many that a
+// CU holds more than two of them: 1023 x 18944 25 to codes and 32 to 16 bits with four turns (640 threads), 19 and 27 with five (512), 21 and 28 with six,
+// 35 and 39 with eight; 655 x 29568 24.7 and 32.7, 24.1 and 31.9 (768 threads), 25.4 and 32.4, 29.8 and 34.8.  (Not everywhere: 787 x 24576 to codes takes 28 with
+// five, 21 with six.)
 template <typename T, typename R, bool Q8>
 static int norm_pick(const NormArgs& a, hipStream_t stream) {
   const int vecs = bpdq_ceil_div(a.d, 8);
