@@ -6,8 +6,8 @@
 // unrounded sum.
 //
 // What bounds it: bytes, and for few rows the launch.  4096 bf16 rows of 8192 with an fp32 residual move 403 MB in 74 us (5.4 TB/s; a large copy
-// reaches 4.9 to 5.3 from card to card); 16 x 3584 takes 3.5 us in a graph, 3.9 alone, 100000 x 128 10.  To codes vector instructions bound it, some 25 a value and 74 % of the
-// busy cycles, conversions to and from fp64 among them: 1023 x 18944 in groups of 128 20 us for 58 MB (2.9 TB/s).
+// reaches 4.9 to 5.3 from card to card); 16 x 3584 takes 3.5 us in a graph, 3.9 alone, 100000 x 128 10.  To codes vector instructions bound it, some 24 a value and 72 % of the
+// busy cycles, conversions to and from fp64 among them: 1023 x 18944 in groups of 128 19.4 us for 58 MB (3.0 TB/s).
 #include "common.h"
 
 namespace bpdq {
