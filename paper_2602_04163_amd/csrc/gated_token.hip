@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kGemvThreads) void gated_token_kernel(LinearArgs a,
     xv[s] = make_float4(v[0], v[1], v[2], v[3]);
   }
   // A bf16 token whose largest value is 2^64 or more, or below 2^-24, is taken times a power of two, in tables made anew: its sums would leave fp32,
-  // or lose bits among fp32's denormals.
+  // or lose bits among fp32's denormals.  (To look costs 0.2 of 4.4 us at 2 x 3584 x 2048, nothing that shows at 14 us.)
   if (bf16) {
     float most = 0.f;
 #pragma unroll
